@@ -88,7 +88,9 @@ EXPORTS = ["pat_decode_query", "pat_decode_init", "pat_load_layer", "pat_load_la
            "pat_decode_destroy", "pat_last_error", "pat_op_packed_weight_bytes", "pat_op_pack_weight",
            "pat_op_packed_act_bytes", "pat_op_pack_act", "pat_op_gemm", "pat_op_gemm_static", "pat_op_gemm_scratch_bytes", "pat_op_gemm_plan", "pat_op_gemm_cut", "pat_op_rmsnorm_pack", "pat_op_embed_stats", "pat_op_pack_act_gain", "pat_op_gemm_norm", "pat_decode_uses_fused_kernel", "pat_op_barrier_probe", "pat_op_argmax",
            "pat_predictor_fit", "pat_predictor_destroy", "pat_predictor_line", "pat_predictor_query", "pat_switch_decide",
-           "pat_kv_move_seconds", "pat_rms_length", "pat_profile_plan"]
+           "pat_kv_move_seconds", "pat_rms_length", "pat_profile_plan",
+           "pat_op_rope_table", "pat_op_kv_append", "pat_op_attn_plan_bytes", "pat_op_attn_scratch_bytes", "pat_op_attn_plan", "pat_op_attn_shared",
+           "pat_op_f8_weight_bytes", "pat_op_f8_scale_bytes", "pat_op_f8_pack_weight", "pat_op_f8_gemm_scratch_bytes", "pat_op_f8_gemm"]
 
 _lib = None
 
@@ -161,6 +163,17 @@ def load_library() -> C.CDLL:
     lib.pat_rms_length.argtypes = [i32p, C.c_int32]
     lib.pat_rms_length.restype = C.c_double
     lib.pat_profile_plan.argtypes = [C.c_int32, C.c_int64, C.c_int64, C.POINTER(pat_plan_point), C.POINTER(C.c_int32)]
+    i32, i64, f32 = C.c_int32, C.c_int64, C.c_float
+    lib.pat_op_rope_table.argtypes = [i64, i32, C.c_double, vp, vp]
+    lib.pat_op_kv_append.argtypes = [vp, i32, i64, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, f32, vp, vp, i32, i32, vp, i32, i32, vp, i64, vp, vp]
+    lib.pat_op_attn_plan.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
+    lib.pat_op_attn_shared.argtypes = [vp, i32, i64, i32, i32, i32, i32, vp, vp, i32, i32, vp, i32, vp, vp, i64, vp, vp]
+    lib.pat_op_f8_pack_weight.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp]
+    lib.pat_op_f8_gemm.argtypes = [vp, vp, i32, i32, vp, i32, i64, i32, vp, i32, i64, i32, vp, vp]
+    for name, n in (("pat_op_attn_plan_bytes", 3), ("pat_op_attn_scratch_bytes", 4), ("pat_op_f8_weight_bytes", 2), ("pat_op_f8_scale_bytes", 2),
+                    ("pat_op_f8_gemm_scratch_bytes", 3)):
+        getattr(lib, name).argtypes = [i32] * n
+        getattr(lib, name).restype = i64
     _lib = lib
     return lib
 
