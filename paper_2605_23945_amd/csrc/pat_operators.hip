@@ -129,13 +129,13 @@ int pat_op_f8_gemm(const void *w_packed, const void *w_scales, int32_t n, int32_
     if (m == 0) return PAT_OK;
     if (!x || !y || !scratch || !aligned(x, size_of(x_type)) || !aligned(y, size_of(y_type)) || !aligned(scratch, 256)) return PAT_EINVAL;
     char *sc = (char *)scratch + f8_operand_bytes(m, k);
-    hipError_t e = launch_f8_pack_act(x, x_type == PAT_F32, ldx, m, k, scratch, sc, (hipStream_t)stream);
-    if (e != hipSuccess) return PAT_EHIP;
     F8Args a{};
     a.w = (const uint4 *)w_packed; a.x = (const uint4 *)scratch; a.ws = (const uint32_t *)w_scales; a.xs = (const uint32_t *)sc;
     a.y = y; a.ldy = ldy; a.n = n; a.m = m; a.Mp = (m + 15) / 16 * 16; a.KB = (k + 127) / 128; a.add = mode == 1;
     a.vec = aligned(y, 4 * size_of(y_type)) && ldy % 4 == 0;
-    return done(launch_f8_gemm(a, y_type == PAT_F32, (hipStream_t)stream));
+    if (m <= 16) return done(launch_f8_gemm_raw(a, x, x_type == PAT_F32, ldx, k, y_type == PAT_F32, (hipStream_t)stream));
+    const hipError_t e = launch_f8_pack_act(x, x_type == PAT_F32, ldx, m, k, scratch, sc, (hipStream_t)stream);
+    return e != hipSuccess ? PAT_EHIP : done(launch_f8_gemm(a, y_type == PAT_F32, compute_units(), (hipStream_t)stream));
 }
 
 }  // extern "C"
