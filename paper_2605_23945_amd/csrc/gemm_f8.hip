@@ -19,71 +19,129 @@ namespace pat {
 namespace {
 
 typedef int v8i_t __attribute__((ext_vector_type(8)));
+typedef short shortx2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short ushortx2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+constexpr uint32_t kInfBits = 0x7F800000u;
 
 // Scale of a block whose largest finite element is amax: biased exponent of the smallest power of two with amax <= 448 2^e.
 // amax = f 2^x with f in [1, 2): 448 = 1.75 * 2^8.  A block of zeros gets 2^0.
-__device__ __forceinline__ int scale_code(float amax)
+__device__ __forceinline__ int scale_code(uint32_t top)
 {
+    const float amax = __uint_as_float(top);
     if (amax == 0.f) return 127;
     int x;
     const float f = frexpf(amax, &x);                          // [0.5, 1): exact for subnormal numbers too
     const int e = x - (f <= 0.875f ? 9 : 8);
     return max(e, -127) + 127;
 }
-// x 2^-e, exactly: 2^(127 - code) is a normal number for every code but 254, which no fp32 element asks for (448 2^e stays below 2^128: e <= 119)
-__device__ __forceinline__ float scaled(float x, int code) { return x * __uint_as_float((uint32_t)(254 - code) << 23); }
-
-__device__ __forceinline__ float finite_abs(float x) { const float a = fabsf(x); return a < INFINITY ? a : 0.f; }     // NaN and infinity count as nothing
-
-// sixteen elements as 8-bit values; what is not finite becomes the format's NaN
-__device__ __forceinline__ uint4 to_f8(const float (&x)[16], int code)
-{
-    uint32_t w[4];
+// Sixteen consecutive elements of a row, as they lie in memory.
+template <typename E> struct Piece;
+template <> struct Piece<float> {
+    uint32_t w[16];
+    __device__ __forceinline__ void load(const float *p)
+    {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        int v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(x[4 * i], code), scaled(x[4 * i + 1], code), 0, false);
-        w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(scaled(x[4 * i + 2], code), scaled(x[4 * i + 3], code), v, true);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (!(fabsf(x[4 * i + j]) < INFINITY)) w[i] |= 0x7Fu << (8 * j);
+        for (int i = 0; i < 4; ++i) {
+            const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-__device__ __forceinline__ float one(const float *p) { return *p; }
-__device__ __forceinline__ float one(const uint16_t *p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ void sixteen(const float *p, float (&x)[16])
-{
+    __device__ __forceinline__ void set(int i, const float *p) { w[i] = p ? __float_as_uint(*p) : 0u; }
+    // the largest magnitude's bits; not below those of infinity if something is not finite
+    __device__ __forceinline__ uint32_t top() const
+    {
+        uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float4 v = reinterpret_cast<const float4 *>(p)[i];
-        x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+        for (int i = 0; i < 16; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
+        return m;
     }
-}
-__device__ __forceinline__ void sixteen(const uint16_t *p, float (&x)[16])
-{
+    __device__ __forceinline__ uint32_t top_finite() const
+    {
+        uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { x[8 * i + 2 * j] = bf16lo(w[j]); x[8 * i + 2 * j + 1] = bf16hi(w[j]); }
+        for (int i = 0; i < 16; ++i) m = max(m, (w[i] & 0x7FFFFFFFu) < 0x7F800000u ? w[i] & 0x7FFFFFFFu : 0u);
+        return m;
     }
-}
+    __device__ __forceinline__ bool finite(int i) const { return (w[i] & 0x7FFFFFFFu) < 0x7F800000u; }
+    __device__ __forceinline__ uint4 to_f8(float scale) const
+    {
+        uint4 o;
+        uint32_t *q = &o.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            shortx2_t v = {0, 0};
+            v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, __uint_as_float(w[4 * i]), __uint_as_float(w[4 * i + 1]), scale, false);
+            v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, __uint_as_float(w[4 * i + 2]), __uint_as_float(w[4 * i + 3]), scale, true);
+            q[i] = __builtin_bit_cast(uint32_t, v);
+        }
+        return o;
+    }
+};
+template <> struct Piece<uint16_t> {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const uint16_t *p)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+    }
+    __device__ __forceinline__ void set(int i, const uint16_t *p)
+    {
+        const uint32_t v = p ? *p : 0u;
+        w[i >> 1] = i & 1 ? w[i >> 1] | v << 16 : v;
+    }
+    __device__ __forceinline__ uint32_t top() const
+    {
+        ushortx2_t m = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(ushortx2_t, w[i] & 0x7FFF7FFFu));
+        return (uint32_t)max(m[0], m[1]) << 16;
+    }
+    __device__ __forceinline__ uint32_t top_finite() const
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m = max(m, finite(i) ? (w[i >> 1] >> (i & 1 ? 16 : 0)) & 0x7FFFu : 0u);
+        return m << 16;
+    }
+    __device__ __forceinline__ bool finite(int i) const { return ((w[i >> 1] >> (i & 1 ? 16 : 0)) & 0x7FFFu) < 0x7F80u; }
+    __device__ __forceinline__ uint4 to_f8(float scale) const
+    {
+        uint4 o;
+        uint32_t *q = &o.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            shortx2_t v = {0, 0};
+            v = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(v, __builtin_bit_cast(bf16x2_t, w[2 * i]), scale, false);
+            v = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(v, __builtin_bit_cast(bf16x2_t, w[2 * i + 1]), scale, true);
+            q[i] = __builtin_bit_cast(uint32_t, v);
+        }
+        return o;
+    }
+};
 // columns c .. c + 15 of a row (NULL: a row of padding), zeros behind column k
 template <typename E>
-__device__ __forceinline__ void load16(const E *row, int c, int k, bool vec, float (&x)[16])
+__device__ __forceinline__ void load16(const E *row, int c, int k, bool vec, Piece<E> &x)
 {
-    if (row && vec && c + 16 <= k) { sixteen(row + c, x); return; }
+    if (row && vec && c + 16 <= k) { x.load(row + c); return; }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = row && c + i < k ? one(row + c + i) : 0.f;
+    for (int i = 0; i < 16; ++i) x.set(i, row && c + i < k ? row + c + i : nullptr);
 }
-__device__ __forceinline__ float amax16(const float (&x)[16])
+// x 2^-e rounded to the format by the conversion instruction, which divides by the scale's power of two; what is not finite becomes the format's NaN
+template <typename E>
+__device__ __forceinline__ uint4 to_f8(const Piece<E> &x, int code, bool all_finite)
 {
-    float m = 0.f;
+    uint4 o = x.to_f8(__uint_as_float((uint32_t)code << 23));
+    if (!all_finite) {
+        uint32_t *q = &o.x;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = fmaxf(m, finite_abs(x[i]));
-    return m;
+        for (int i = 0; i < 16; ++i)
+            if (!x.finite(i)) q[i >> 2] |= 0x7Fu << (8 * (i & 3));
+    }
+    return o;
 }
 
 // Activations: eight lanes hold a row's block; a workgroup two blocks of 16 rows.  Scales [KB4][16 tiles][4]: a word holds four
@@ -93,13 +151,15 @@ __global__ __launch_bounds__(256) void f8_pack_act_kernel(const E *x, int64_t ld
 {
     const int r = threadIdx.x >> 3 & 15, piece = threadIdx.x & 7, kb = blockIdx.x * 2 + (threadIdx.x >> 7), tile = blockIdx.y, row = tile * 16 + r;
     if (kb >= KB) return;
-    float v[16];
+    Piece<E> v;
     load16(row < m ? x + (int64_t)row * ld : nullptr, kb * 128 + piece * 16, k, vec, v);
-    float a = amax16(v);
+    uint32_t a = v.top();
+    const bool fin = !__any(a >= kInfBits);
+    if (!fin) a = v.top_finite();
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) a = fmaxf(a, __shfl_xor(a, o, 64));
+    for (int o = 1; o < 8; o <<= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o, 64));
     const int code = scale_code(a);
-    packed[((int64_t)tile * KB + kb) * 128 + (piece >> 2) * 64 + (piece & 3) * 16 + r] = to_f8(v, code);
+    packed[((int64_t)tile * KB + kb) * 128 + (piece >> 2) * 64 + (piece & 3) * 16 + r] = to_f8(v, code, fin);
     if (piece == 0) scales[((int64_t)(kb >> 2) * Mp + row) * 4 + (kb & 3)] = (uint8_t)code;
 }
 
@@ -107,23 +167,27 @@ __global__ __launch_bounds__(256) void f8_pack_act_kernel(const E *x, int64_t ld
 template <typename E>
 __global__ __launch_bounds__(256) void f8_pack_weight_kernel(const E *w, int64_t ld, int n, int k, int KB, bool vec, uint4 *packed, uint8_t *scales, int KB4)
 {
-    __shared__ float top[4];
+    __shared__ uint32_t top[4];
     const int kb = blockIdx.x, nb = blockIdx.y, piece = threadIdx.x & 7;
-    float v[4][16], a = 0.f;
+    Piece<E> v[4];
+    uint32_t a = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int row = nb * 128 + i * 32 + (threadIdx.x >> 3);
         load16(row < n ? w + (int64_t)row * ld : nullptr, kb * 128 + piece * 16, k, vec, v[i]);
-        a = fmaxf(a, amax16(v[i]));
+        a = max(a, v[i].top());
     }
-    a = wave_max(a);
+    const bool fin = !__any(a >= kInfBits);
+    if (!fin) a = max(max(v[0].top_finite(), v[1].top_finite()), max(v[2].top_finite(), v[3].top_finite()));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o, 64));
     if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = a;
     __syncthreads();
-    const int code = scale_code(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+    const int code = scale_code(max(max(top[0], top[1]), max(top[2], top[3])));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int row = nb * 128 + i * 32 + (threadIdx.x >> 3), tile = row >> 4;
-        if (tile < (n + 15) / 16) packed[((int64_t)tile * KB + kb) * 128 + (piece >> 2) * 64 + (piece & 3) * 16 + (row & 15)] = to_f8(v[i], code);
+        if (tile < (n + 15) / 16) packed[((int64_t)tile * KB + kb) * 128 + (piece >> 2) * 64 + (piece & 3) * 16 + (row & 15)] = to_f8(v[i], code, fin);
     }
     if (threadIdx.x == 0) scales[((int64_t)nb * KB4 + (kb >> 2)) * 4 + (kb & 3)] = (uint8_t)code;
 }
@@ -139,7 +203,6 @@ __device__ __forceinline__ floatx4_t mfma_f8(v8i_t a, v8i_t b, floatx4_t c, int 
 // eight 8-bit values as bf16, exactly
 __device__ __forceinline__ bf16x8_t widen8(int lo, int hi)
 {
-    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
     const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
     const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
     return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
@@ -185,74 +248,102 @@ __device__ __forceinline__ void emit(const F8Args &a, int m, int n0, floatx4_t v
 }
 
 // ---- few rows: weights streamed once, straight into registers ------------------------------------------------------
-// A workgroup holds one tile of 16 weight rows; its eight waves take the blocks of columns in turn (wave w: w, w + 8, ...), four at a time, so
-// that 8 KiB of weights are in flight per wave, and their sums meet in LDS, added in wave order.  Up to 16 rows (RAW) every wave
-// brings x to its 8-bit form itself, in the registers the product reads it from: lanes r, r + 16, r + 32 and r + 48 hold row r's block, no launch, no
-// scratch and no barrier precede the stream.  Above, x comes packed.
-constexpr int kStreamWaves = 8, kStreamAhead = 4;
+// A workgroup holds TN tiles of 16 weight rows; its eight waves take the blocks of columns in turn (wave w: w, w + 8, ...) and their
+// sums meet in LDS, added in wave order.  A wave keeps three blocks' operands in registers (two above 32 rows), all but one of them on their way: a block's weights and its part of x
+// are requested together, since loads arrive in order.  Up to 16 rows (RAW) every wave brings x to its 8-bit form
+// itself, in the registers the product reads it from: lanes r, r + 16, r + 32 and r + 48 hold row r's block; no launch, no scratch and no barrier
+// precede the stream.  Above, x comes packed.
+constexpr int kStreamWaves = 8;
 
-__device__ __forceinline__ uint4 load_once(const uint4 *p)
-{
-    const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
-    return make_uint4(v[0], v[1], v[2], v[3]);
-}
+__device__ __forceinline__ v8i_t both(u32x4_t a, u32x4_t b) { return v8i_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]}; }
 
-template <int MB, bool RAW, typename X, typename E>
+template <int MB, int TN, bool RAW, typename X, typename E>
 __global__ __launch_bounds__(kStreamWaves * 64) void f8_stream_kernel(F8Args a, const X *xraw, int64_t ldx, int k, bool xvec)
 {
-    __shared__ floatx4_t red[kStreamWaves][MB][64];
+    __shared__ floatx4_t red[kStreamWaves][MB * TN][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-    const int KB = a.KB, KB4 = (KB + 3) / 4, nt = blockIdx.x;
-    const uint4 *w = a.w + (int64_t)nt * KB * 128 + lane;
-    const uint32_t *ws = a.ws + (int64_t)(nt >> 3) * KB4;
-    floatx4_t acc[MB] = {};
-    for (int k0 = wave; k0 < KB; k0 += kStreamWaves * kStreamAhead) {
-        uint4 wf[kStreamAhead][2];
+    const int KB = a.KB, KB4 = (KB + 3) / 4, nt0 = blockIdx.x * TN, NT = (a.n + 15) / 16;
+    const u32x4_t *w[TN];
+    const uint32_t *ws[TN];
 #pragma unroll
-        for (int u = 0; u < kStreamAhead; ++u) {
-            const int kb = min(k0 + u * kStreamWaves, KB - 1);
-            wf[u][0] = load_once(w + kb * 128); wf[u][1] = load_once(w + kb * 128 + 64);
-        }
+    for (int t = 0; t < TN; ++t) {
+        const int nt = min(nt0 + t, NT - 1);
+        w[t] = reinterpret_cast<const u32x4_t *>(a.w) + (int64_t)nt * KB * 128 + lane;
+        ws[t] = a.ws + (int64_t)(nt >> 3) * KB4;
+    }
+    const X *row = xraw + (int64_t)min(col, a.m - 1) * ldx;
+    struct Packed { u32x4_t f[MB][2]; int s[MB]; };
+    struct Raw { Piece<X> lo, hi; };
+    struct Block { u32x4_t f[TN][2]; typename std::conditional<RAW, Raw, Packed>::type x; };
+    auto load = [&](Block &b, int kb) {
+        if (kb >= KB) return;
+        if constexpr (RAW) {
+            const int c = kb * 128 + g * 16;
+            if (xvec && (kb + 1) * 128 <= k) { b.x.lo.load(row + c); b.x.hi.load(row + c + 64); }
+            else { load16(row, c, k, false, b.x.lo); load16(row, c + 64, k, false, b.x.hi); }
+        } else {
 #pragma unroll
-        for (int u = 0; u < kStreamAhead; ++u) {
-            const int kb = k0 + u * kStreamWaves;
-            if (kb >= KB) break;
-            const int sw = ws[kb >> 2] >> (8 * (kb & 3));
-            const v8i_t wv = both(wf[u][0], wf[u][1]);
-#pragma unroll
-            for (int t = 0; t < MB; ++t) {
-                v8i_t xv;
-                int sx;
-                if (RAW) {
-                    float lo[16], hi[16];
-                    const X *row = col < a.m ? xraw + (int64_t)col * ldx : nullptr;
-                    load16(row, kb * 128 + g * 16, k, xvec, lo);
-                    load16(row, kb * 128 + 64 + g * 16, k, xvec, hi);
-                    float top = fmaxf(amax16(lo), amax16(hi));
-                    top = fmaxf(top, __shfl_xor(top, 16, 64));
-                    top = fmaxf(top, __shfl_xor(top, 32, 64));
-                    sx = scale_code(top);
-                    xv = both(to_f8(lo, sx), to_f8(hi, sx));
-                } else {
-                    const uint4 *x = a.x + ((int64_t)t * KB + kb) * 128 + lane;
-                    xv = both(x[0], x[64]);
-                    sx = a.xs[(int64_t)(kb >> 2) * a.Mp + t * 16 + col] >> (8 * (kb & 3));
-                }
-                acc[t] = sizeof(E) == 4 ? mfma_wide(wv, xv, acc[t], sw, sx) : mfma_f8<0>(wv, xv, acc[t], sw, sx);
+            for (int i = 0; i < MB; ++i) {
+                const u32x4_t *x = reinterpret_cast<const u32x4_t *>(a.x) + ((int64_t)i * KB + kb) * 128 + lane;
+                b.x.f[i][0] = x[0]; b.x.f[i][1] = x[64];
+                b.x.s[i] = a.xs[(int64_t)(kb >> 2) * a.Mp + i * 16 + col] >> (8 * (kb & 3));
             }
         }
-    }
 #pragma unroll
-    for (int t = 0; t < MB; ++t) red[wave][t][lane] = acc[t];
+        for (int t = 0; t < TN; ++t) { b.f[t][0] = __builtin_nontemporal_load(w[t] + kb * 128); b.f[t][1] = __builtin_nontemporal_load(w[t] + kb * 128 + 64); }
+    };
+    floatx4_t acc[MB][TN] = {};
+    auto multiply = [&](const Block &b, int kb) {
+        if (kb >= KB) return;
+        int sw[TN];
+#pragma unroll
+        for (int t = 0; t < TN; ++t) sw[t] = ws[t][kb >> 2] >> (8 * (kb & 3));
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+            v8i_t xv;
+            int sx;
+            if constexpr (RAW) {                               // columns behind the batch repeat its last row; their results are dropped
+                uint32_t top = max(b.x.lo.top(), b.x.hi.top());
+                const bool fin = !__any(top >= kInfBits);
+                if (!fin) top = max(b.x.lo.top_finite(), b.x.hi.top_finite());
+                top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+                top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+                sx = scale_code(top);
+                xv = both(to_f8(b.x.lo, sx, fin), to_f8(b.x.hi, sx, fin));
+            } else {
+                xv = both(b.x.f[i][0], b.x.f[i][1]);
+                sx = b.x.s[i];
+            }
+#pragma unroll
+            for (int t = 0; t < TN; ++t) {
+                const v8i_t wv = both(b.f[t][0], b.f[t][1]);
+                acc[i][t] = sizeof(E) == 4 ? mfma_wide(wv, xv, acc[i][t], sw[t], sx) : mfma_f8<0>(wv, xv, acc[i][t], sw[t], sx);
+            }
+        }
+    };
+    constexpr int W = kStreamWaves, R = MB > 2 ? 2 : 3;        // blocks in registers: with more of x, one on its way
+    Block b[R];
+#pragma unroll
+    for (int i = 0; i < R - 1; ++i) load(b[i], wave + i * W);
+    for (int kb = wave; kb < KB; kb += R * W)
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            load(b[(i + R - 1) % R], kb + (i + R - 1) * W);
+            multiply(b[i], kb + i * W);
+        }
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int t = 0; t < TN; ++t) red[wave][i * TN + t][lane] = acc[i][t];
     __syncthreads();
-    if (wave < MB) {
-        floatx4_t v = red[0][wave][lane];
+    for (int x = wave; x < MB * TN; x += W) {
+        floatx4_t v = red[0][x][lane];
 #pragma unroll
-        for (int i = 1; i < kStreamWaves; ++i) {
-            const floatx4_t u = red[i][wave][lane];
+        for (int i = 1; i < W; ++i) {
+            const floatx4_t u = red[i][x][lane];
             v[0] += u[0]; v[1] += u[1]; v[2] += u[2]; v[3] += u[3];
         }
-        emit<E>(a, wave * 16 + col, nt * 16 + g * 4, v);
+        emit<E>(a, x / TN * 16 + col, (nt0 + x % TN) * 16 + g * 4, v);
     }
 }
 
@@ -262,27 +353,31 @@ __global__ __launch_bounds__(kStreamWaves * 64) void f8_stream_kernel(F8Args a, 
 // registers, a block of columns ahead.  Before the last weight tile of a block all waves meet: what the next block needs has arrived, and
 // the stage just read is requested anew.
 template <int TN, int TM, typename E>
-__global__ __launch_bounds__(256) void f8_tile_kernel(F8Args a, int nblk, int mblk)
+__global__ __launch_bounds__(256, TN * TM * (sizeof(E) == 4 ? 2 : 1) <= 32 ? 2 : 1) void f8_tile_kernel(F8Args a, int nblk, int mblk, int slices)
 {
     constexpr int kStage = TN * 2048, NJ = TN / 2;             // load instructions of a wave per stage
+    constexpr int kAhead = 3;                                  // weight tiles on their way from LDS: one tile's products are shorter than its read
     constexpr bool WIDE = sizeof(E) == 4;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-    const int KB = a.KB, KB4 = (KB + 3) / 4, NT = (a.n + 15) / 16, MT = a.Mp / 16;
+    const int KB4 = (a.KB + 3) / 4, NT = (a.n + 15) / 16, MT = a.Mp / 16;
     // workgroups of an XCD (index mod 8) take neighbouring tiles: four columns of batch blocks, then the next weights
-    int nb, mb;
+    int nb, mb, sl;
     {
-        const int T = nblk * mblk, xcd = blockIdx.x & 7, q = T >> 3, r = T & 7;
-        const int L = xcd * q + min(xcd, r) + (blockIdx.x >> 3);
+        const int T = nblk * mblk * slices, xcd = blockIdx.x & 7, q = T >> 3, r = T & 7;
+        int L = xcd * q + min(xcd, r) + (blockIdx.x >> 3);
+        sl = L / (nblk * mblk);
+        L -= sl * nblk * mblk;
         const int band = L / (nblk * 4), w = min(4, mblk - band * 4), i = L - band * nblk * 4;
         nb = i / w; mb = band * 4 + i - nb * w;
     }
+    const int first = sl * a.KB / slices, KB = (sl + 1) * a.KB / slices;      // this workgroup's blocks of columns
     const uint32_t lds0 = lds_offset(lds);
     const char *wsrc[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
         const int idx = wave * NJ + j;
-        wsrc[j] = reinterpret_cast<const char *>(a.w) + (int64_t)min(nb * TN + (idx >> 1), NT - 1) * KB * 2048 + (idx & 1) * 1024;
+        wsrc[j] = reinterpret_cast<const char *>(a.w) + (int64_t)min(nb * TN + (idx >> 1), NT - 1) * a.KB * 2048 + (idx & 1) * 1024;
     }
     auto fetch = [&](int kb) {
 #pragma unroll
@@ -293,7 +388,7 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Args a, int nblk, int mb
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int mt = min((mb * 4 + wave) * TM + i, MT - 1);
-        xsrc[i] = a.x + (int64_t)mt * KB * 128 + lane;
+        xsrc[i] = a.x + (int64_t)mt * a.KB * 128 + lane;
         xss[i] = a.xs + mt * 16 + col;
     }
     const uint32_t *wss = a.ws + (int64_t)(nb * TN >> 3) * KB4, *wss2 = a.ws + (int64_t)min((nb * TN + TN - 1) >> 3, (NT - 1) >> 3) * KB4;
@@ -318,14 +413,15 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Args a, int nblk, int mb
     };
     floatx4_t acc[TN][TM] = {};
     Batch b0, b1;
-    u32x4_t wf[2][2];
-    fetch(0);
-    load_batch(b0, 0);
+    u32x4_t wf[4][2];
+    fetch(first);
+    load_batch(b0, first);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     pin(b0);
     asm volatile("s_barrier" ::: "memory");
-    fetch(1);
-    weight(0, 0, wf[0]);
+    fetch(first + 1);
+#pragma unroll
+    for (int t = 0; t < kAhead; ++t) weight(first, t, wf[t]);
     // No branch in here: the compiler moves matrix products past one.  Behind the last block the last one's operands are read again, for nothing.
     auto step = [&](int kb, Batch &b, Batch &next) {
         load_batch(next, min(kb + 1, KB - 1));
@@ -334,15 +430,15 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Args a, int nblk, int mb
 #pragma unroll
         for (int t = 0; t < TN; ++t) {
             __builtin_amdgcn_sched_barrier(0);                 // or all of the block's weights are read ahead, into registers that the sums need
-            if (t + 1 < TN) weight(kb, t + 1, wf[(t + 1) & 1]);
-            else {
+            if (t + kAhead == TN) {
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
                 pin(next);
                 asm volatile("s_barrier" ::: "memory");
                 fetch(kb + 2);
-                weight(kb + 1, 0, wf[(t + 1) & 1]);
             }
-            const u32x4_t f0 = wf[t & 1][0], f1 = wf[t & 1][1];
+            if (t + kAhead < TN) weight(kb, t + kAhead, wf[(t + kAhead) & 3]);
+            else weight(kb + 1, t + kAhead - TN, wf[(t + kAhead) & 3]);
+            const u32x4_t f0 = wf[t & 3][0], f1 = wf[t & 3][1];
             const v8i_t wv = v8i_t{(int)f0[0], (int)f0[1], (int)f0[2], (int)f0[3], (int)f1[0], (int)f1[1], (int)f1[2], (int)f1[3]};
             const int s = t < edge ? sw : sw2;
 #pragma unroll
@@ -354,11 +450,20 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Args a, int nblk, int mb
             }
         }
     };
-    static_assert(TN % 2 == 0, "the next block's first weights land where this step's begin");
-    int kb = 0;
-    for (; kb + 1 < KB; kb += 2) { step(kb, b0, b1); step(kb + 1, b1, b0); }
-    if (kb < KB) step(kb, b0, b1);
+    static_assert(TN % 4 == 0, "the next block's first weights land where this step's begin");
+    for (int kb = first; kb < KB; ++kb) { step(kb, b0, b1); b0 = b1; }      // two steps a turn, and the compiler moves the sums about
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // nothing may arrive in LDS that has gone to another workgroup
+    if (slices > 1) {                                          // fp32 sums of the slice: [slice][batch row][weight row]
+        float *part = a.part + (int64_t)sl * a.Mp * NT * 16;
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int mt = (mb * 4 + wave) * TM + i, nt = nb * TN + t;
+                if (mt < MT && nt < NT) *reinterpret_cast<floatx4_t *>(part + ((int64_t)(mt * 16 + col) * NT + nt) * 16 + g * 4) = acc[t][i];
+            }
+        return;
+    }
 #pragma unroll
     for (int t = 0; t < TN; ++t)
 #pragma unroll
@@ -368,41 +473,85 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Args a, int nblk, int mb
         }
 }
 
-template <int TN, int TM, typename E>
-hipError_t launch_tile(const F8Args &a, hipStream_t s)
+// the slices' sums, added in their order
+template <typename E>
+__global__ __launch_bounds__(256) void f8_join_kernel(F8Args a, int slices)
 {
-    const int nblk = ((a.n + 15) / 16 + TN - 1) / TN, mblk = (a.Mp / 16 + 4 * TM - 1) / (4 * TM);
-    f8_tile_kernel<TN, TM, E><<<(unsigned)(nblk * mblk), 256, 2 * TN * 2048, s>>>(a, nblk, mblk);
+    const int NT = (a.n + 15) / 16;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (int64_t)a.m * NT * 4;
+    if (i >= per) return;
+    const int m = (int)(i / (NT * 4)), n4 = (int)(i - (int64_t)m * NT * 4);
+    const floatx4_t *p = reinterpret_cast<const floatx4_t *>(a.part) + i;
+    floatx4_t v = p[0];
+    for (int s = 1; s < slices; ++s) {
+        const floatx4_t u = p[(int64_t)s * a.Mp * NT * 4];
+        v[0] += u[0]; v[1] += u[1]; v[2] += u[2]; v[3] += u[3];
+    }
+    emit<E>(a, m, n4 * 4, v);
+}
+
+template <int TN, int TM, typename E>
+hipError_t launch_tile(const F8Args &a, int slices, hipStream_t s)
+{
+    const int NT = (a.n + 15) / 16, nblk = (NT + TN - 1) / TN, mblk = (a.Mp / 16 + 4 * TM - 1) / (4 * TM);
+    f8_tile_kernel<TN, TM, E><<<(unsigned)(nblk * mblk * slices), 256, 2 * TN * 2048, s>>>(a, nblk, mblk, slices);
+    if (slices > 1) f8_join_kernel<E><<<(unsigned)(((int64_t)a.m * NT * 4 + 255) / 256), 256, 0, s>>>(a, slices);
+    return hipGetLastError();
+}
+
+// tiles of a workgroup: as few as leave one workgroup per compute unit
+template <int MB, bool RAW, typename X, typename E>
+hipError_t launch_stream(const F8Args &a, const X *x, int64_t ldx, int k, bool vec, hipStream_t s)
+{
+    const int NT = (a.n + 15) / 16;
+    if (NT <= 320) f8_stream_kernel<MB, 1, RAW, X, E><<<NT, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
+    else if (NT <= 512) f8_stream_kernel<MB, 2, RAW, X, E><<<(NT + 1) / 2, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
+    else f8_stream_kernel<MB, 3, RAW, X, E><<<(NT + 2) / 3, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
     return hipGetLastError();
 }
 
 template <typename E>
-hipError_t launch_product(const F8Args &a, int n_cu, hipStream_t s)
+hipError_t launch_product(const F8Args &a, hipStream_t s)
 {
-    const int NT = (a.n + 15) / 16, MT = a.Mp / 16;
+    const int MT = a.Mp / 16;
     if (MT <= 4) {
         switch (MT) {
-        case 1: f8_stream_kernel<1, false, float, E><<<NT, kStreamWaves * 64, 0, s>>>(a, nullptr, 0, 0, false); break;
-        case 2: f8_stream_kernel<2, false, float, E><<<NT, kStreamWaves * 64, 0, s>>>(a, nullptr, 0, 0, false); break;
-        case 3: f8_stream_kernel<3, false, float, E><<<NT, kStreamWaves * 64, 0, s>>>(a, nullptr, 0, 0, false); break;
-        default: f8_stream_kernel<4, false, float, E><<<NT, kStreamWaves * 64, 0, s>>>(a, nullptr, 0, 0, false); break;
+        case 2: return launch_stream<2, false, float, E>(a, nullptr, 0, 0, false, s);
+        case 3: return launch_stream<3, false, float, E>(a, nullptr, 0, 0, false, s);
+        default: return launch_stream<4, false, float, E>(a, nullptr, 0, 0, false, s);
         }
-        return hipGetLastError();
     }
-    if constexpr (sizeof(E) == 4) return MT <= 8 ? launch_tile<4, 2, E>(a, s) : launch_tile<4, 4, E>(a, s);
-    else {
-    if (MT <= 8) return launch_tile<8, 2, E>(a, s);
-    // workgroups in rounds of the compute units: the height that ends the last round soonest
-    const int mblk = (MT + 15) / 16;
-    auto cost = [&](int tn, int per_cu) { const int64_t wg = (int64_t)((NT + tn - 1) / tn) * mblk, slots = (int64_t)n_cu * per_cu; return (wg + slots - 1) / slots * tn * per_cu; };
-    const int64_t c6 = cost(6, 2), c8 = cost(8, 2), c12 = cost(12, 1), c16 = cost(16, 1);
-    if (c16 <= c12 && c16 <= c8 && c16 <= c6) return launch_tile<16, 4, E>(a, s);
-    if (c12 <= c8 && c12 <= c6) return launch_tile<12, 4, E>(a, s);
-    return c8 <= c6 ? launch_tile<8, 4, E>(a, s) : launch_tile<6, 4, E>(a, s);
+    const F8Tile t = f8_tile(a.n, a.m, a.KB);
+    if constexpr (sizeof(E) == 4) return t.TM == 2 ? launch_tile<4, 2, E>(a, t.slices, s) : launch_tile<4, 4, E>(a, t.slices, s);
+    else if (t.TM == 2) return launch_tile<8, 2, E>(a, t.slices, s);
+    else switch (t.TN) {
+    case 16: return launch_tile<16, 4, E>(a, t.slices, s);
+    case 12: return launch_tile<12, 4, E>(a, t.slices, s);
+    case 8: return launch_tile<8, 4, E>(a, t.slices, s);
+    default: return launch_tile<4, 4, E>(a, t.slices, s);
     }
 }
 
 }  // namespace
+
+// workgroups in rounds of the compute units: the height and the number of slices that end the last round soonest
+F8Tile f8_tile(int n, int m, int KB)
+{
+    const int NT = (n + 15) / 16, MT = (m + 15) / 16, TM = MT <= 8 ? 2 : 4, mblk = (MT + 4 * TM - 1) / (4 * TM);
+    F8Tile best{0, TM, 1};
+    double least = 1e30;
+    for (int tn : {16, 12, 8, 4}) {
+        if (TM == 2 && tn != 8) continue;
+        for (int sl = 1; sl <= 8 && sl * 4 <= KB; ++sl) {
+            const int64_t wg = (int64_t)((NT + tn - 1) / tn) * mblk * sl;
+            const double rounds = (double)((wg + 255) / 256);
+            const double cost = rounds * ((double)((KB + sl - 1) / sl) * (700.0 + tn * TM * 48.0) + 5000.0) + (sl > 1 ? 6000.0 + (double)m * n * sl * 8 / 2500.0 : 0.0);
+            if (cost < least) { least = cost; best.TN = tn; best.slices = sl; }
+        }
+    }
+    if (best.TN == 0) best.TN = 8;
+    return best;
+}
 
 hipError_t launch_f8_pack_act(const void *x, bool f32, int64_t ld, int m, int k, void *packed, void *scales, hipStream_t s)
 {
@@ -424,20 +573,13 @@ hipError_t launch_f8_pack_weight(const void *w, bool f32, int64_t ld, int n, int
     return hipGetLastError();
 }
 
-hipError_t launch_f8_gemm(const F8Args &a, bool f32, int n_cu, hipStream_t s) { return f32 ? launch_product<float>(a, n_cu, s) : launch_product<uint16_t>(a, n_cu, s); }
+hipError_t launch_f8_gemm(const F8Args &a, bool f32, hipStream_t s) { return f32 ? launch_product<float>(a, s) : launch_product<uint16_t>(a, s); }
 
 hipError_t launch_f8_gemm_raw(const F8Args &a, const void *x, bool x32, int64_t ldx, int k, bool y32, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((a.n + 15) / 16);
     const bool vec = ((uintptr_t)x & 15) == 0 && ldx * (x32 ? 4 : 2) % 16 == 0;
-    if (x32) {
-        if (y32) f8_stream_kernel<1, true, float, float><<<grid, kStreamWaves * 64, 0, s>>>(a, (const float *)x, ldx, k, vec);
-        else f8_stream_kernel<1, true, float, uint16_t><<<grid, kStreamWaves * 64, 0, s>>>(a, (const float *)x, ldx, k, vec);
-    } else {
-        if (y32) f8_stream_kernel<1, true, uint16_t, float><<<grid, kStreamWaves * 64, 0, s>>>(a, (const uint16_t *)x, ldx, k, vec);
-        else f8_stream_kernel<1, true, uint16_t, uint16_t><<<grid, kStreamWaves * 64, 0, s>>>(a, (const uint16_t *)x, ldx, k, vec);
-    }
-    return hipGetLastError();
+    if (x32) return y32 ? launch_stream<1, true, float, float>(a, (const float *)x, ldx, k, vec, s) : launch_stream<1, true, float, uint16_t>(a, (const float *)x, ldx, k, vec, s);
+    return y32 ? launch_stream<1, true, uint16_t, float>(a, (const uint16_t *)x, ldx, k, vec, s) : launch_stream<1, true, uint16_t, uint16_t>(a, (const uint16_t *)x, ldx, k, vec, s);
 }
 
 }  // namespace pat

@@ -116,9 +116,11 @@ int pat_op_f8_pack_weight(const void *w, int32_t type, int64_t ld, int32_t n, in
 
 static bool batch_ok(int32_t n, int32_t k, int32_t m) { return product_ok(n, k) && m >= 0 && m <= (1 << 19); }
 
+static int64_t part_offset(int32_t m, int32_t k) { return (f8_operand_bytes(m, k) + f8_act_scale_bytes(m, k) + 255) / 256 * 256; }
+
 int64_t pat_op_f8_gemm_scratch_bytes(int32_t n, int32_t k, int32_t m)
 {
-    return batch_ok(n, k, m) ? f8_operand_bytes(m, k) + f8_act_scale_bytes(m, k) : -1;
+    return batch_ok(n, k, m) ? part_offset(m, k) + f8_part_bytes(n, m, k) : -1;
 }
 
 int pat_op_f8_gemm(const void *w_packed, const void *w_scales, int32_t n, int32_t k, const void *x, int32_t x_type, int64_t ldx, int32_t m, void *y,
@@ -132,10 +134,11 @@ int pat_op_f8_gemm(const void *w_packed, const void *w_scales, int32_t n, int32_
     F8Args a{};
     a.w = (const uint4 *)w_packed; a.x = (const uint4 *)scratch; a.ws = (const uint32_t *)w_scales; a.xs = (const uint32_t *)sc;
     a.y = y; a.ldy = ldy; a.n = n; a.m = m; a.Mp = (m + 15) / 16 * 16; a.KB = (k + 127) / 128; a.add = mode == 1;
+    a.part = (float *)((char *)scratch + part_offset(m, k));
     a.vec = aligned(y, 4 * size_of(y_type)) && ldy % 4 == 0;
     if (m <= 16) return done(launch_f8_gemm_raw(a, x, x_type == PAT_F32, ldx, k, y_type == PAT_F32, (hipStream_t)stream));
     const hipError_t e = launch_f8_pack_act(x, x_type == PAT_F32, ldx, m, k, scratch, sc, (hipStream_t)stream);
-    return e != hipSuccess ? PAT_EHIP : done(launch_f8_gemm(a, y_type == PAT_F32, compute_units(), (hipStream_t)stream));
+    return e != hipSuccess ? PAT_EHIP : done(launch_f8_gemm(a, y_type == PAT_F32, (hipStream_t)stream));
 }
 
 }  // extern "C"

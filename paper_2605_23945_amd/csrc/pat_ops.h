@@ -82,10 +82,19 @@ struct F8Args {
     int64_t ldy;
     int n, m, Mp, KB;          // Mp: m up to a multiple of 16; KB: blocks of 128 columns
     bool add, vec;             // y += ; rows n .. n + 3 of y by one store
+    float *part;               // sums of K slices [slice][Mp][16-row tiles of n][16], where f8_tile has more than one
 };
+struct F8Tile { int TN, TM, slices; };      // tiles of weight rows per workgroup, of batch rows per wave, cuts of K
+F8Tile f8_tile(int n, int m, int KB);
+inline int64_t f8_part_bytes(int n, int m, int k)
+{
+    if (m <= 64) return 0;
+    const F8Tile t = f8_tile(n, m, (k + 127) / 128);
+    return t.slices > 1 ? (int64_t)t.slices * ((m + 15) / 16 * 16) * ((n + 15) / 16 * 16) * 4 : 0;
+}
 hipError_t launch_f8_pack_act(const void *x, bool f32, int64_t ld, int m, int k, void *packed, void *scales, hipStream_t s);
 hipError_t launch_f8_pack_weight(const void *w, bool f32, int64_t ld, int n, int k, void *packed, void *scales, hipStream_t s);
-hipError_t launch_f8_gemm(const F8Args &a, bool f32, int n_cu, hipStream_t s);
+hipError_t launch_f8_gemm(const F8Args &a, bool f32, hipStream_t s);
 // up to 16 rows: x as it is, brought to its 8-bit form by the product's own waves (F8Args::x, xs unused)
 hipError_t launch_f8_gemm_raw(const F8Args &a, const void *x, bool x32, int64_t ldx, int k, bool y32, hipStream_t s);
 
