@@ -145,12 +145,11 @@ __device__ __forceinline__ uint4 to_f8(const Piece<E> &x, int code, bool all_fin
 }
 
 // Activations: eight lanes hold a row's block; a workgroup two blocks of 16 rows.  Scales [KB4][16 tiles][4]: a word holds four
-// blocks of one row, which is how the products' lanes load them.
+// blocks of one row, which is how the products' lanes load them; blocks are padded to that with zeros.
 template <typename E>
-__global__ __launch_bounds__(256) void f8_pack_act_kernel(const E *x, int64_t ld, int m, int k, int KB, bool vec, uint4 *packed, uint8_t *scales, int Mp)
+__global__ __launch_bounds__(256) void f8_pack_act_kernel(const E *x, int64_t ld, int m, int k, int KB4, bool vec, uint4 *packed, uint8_t *scales, int Mp)
 {
     const int r = threadIdx.x >> 3 & 15, piece = threadIdx.x & 7, kb = blockIdx.x * 2 + (threadIdx.x >> 7), tile = blockIdx.y, row = tile * 16 + r;
-    if (kb >= KB) return;
     Piece<E> v;
     load16(row < m ? x + (int64_t)row * ld : nullptr, kb * 128 + piece * 16, k, vec, v);
     uint32_t a = v.top();
@@ -159,7 +158,7 @@ __global__ __launch_bounds__(256) void f8_pack_act_kernel(const E *x, int64_t ld
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o, 64));
     const int code = scale_code(a);
-    packed[((int64_t)tile * KB + kb) * 128 + (piece >> 2) * 64 + (piece & 3) * 16 + r] = to_f8(v, code, fin);
+    packed[((int64_t)tile * KB4 * 4 + kb) * 128 + (piece >> 2) * 64 + (piece & 3) * 16 + r] = to_f8(v, code, fin);
     if (piece == 0) scales[((int64_t)(kb >> 2) * Mp + row) * 4 + (kb & 3)] = (uint8_t)code;
 }
 
@@ -284,7 +283,7 @@ __global__ __launch_bounds__(kStreamWaves * 64) void f8_stream_kernel(F8Args a, 
         } else {
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
-                const u32x4_t *x = reinterpret_cast<const u32x4_t *>(a.x) + ((int64_t)i * KB + kb) * 128 + lane;
+                const u32x4_t *x = reinterpret_cast<const u32x4_t *>(a.x) + ((int64_t)i * KB4 * 4 + kb) * 128 + lane;
                 b.x.f[i][0] = x[0]; b.x.f[i][1] = x[64];
                 b.x.s[i] = a.xs[(int64_t)(kb >> 2) * a.Mp + i * 16 + col] >> (8 * (kb & 3));
             }
@@ -348,17 +347,21 @@ __global__ __launch_bounds__(kStreamWaves * 64) void f8_stream_kernel(F8Args a, 
 }
 
 // ---- many rows: tiles on the matrix cores ------------------------------------------------------------------------------
-// A workgroup holds TN tiles of 16 weight rows and 4 TM tiles of 16 batch rows, a wave all TN and TM of the batch's: weights go through LDS
-// (asynchronous loads, two stages of TN x 2 KiB), where the four waves share them; the batch's tiles are one wave's alone and go straight to
-// registers, a block of columns ahead.  Before the last weight tile of a block all waves meet: what the next block needs has arrived, and
-// the stage just read is requested anew.
-template <int TN, int TM, typename E>
-__global__ __launch_bounds__(256, TN * TM * (sizeof(E) == 4 ? 2 : 1) <= 32 ? 2 : 1) void f8_tile_kernel(F8Args a, int nblk, int mblk, int slices)
+// A workgroup holds TN tiles of 16 weight rows and 8 tiles of 16 batch rows, a wave all TN and two of the batch's: weights go through LDS
+// (asynchronous loads, S stages of TN x 2 KiB), where the four waves share them; the batch's tiles are one wave's alone and go straight to
+// registers, three blocks of columns ahead (x has just been written, so it comes from beyond the XCD's own L2).  Towards the end
+// of a block all waves meet: the next block's weights have arrived, and the stage just read is requested anew.  Loads arrive in order,
+// so a wave waits for its weights by the number of loads that it has issued since.
+// The loop takes four blocks a turn, which one word of scales covers; K is padded to that with blocks of x that are zero.  There is no branch
+// in it: the compiler moves matrix products past one.
+constexpr int kBatchTiles = 2;      // four, and workgroups of 256 rows: 287 us where two take 286 (5003 x 7168 x 8192), more at every smaller batch
+template <int TN, int S, typename E>
+__global__ __launch_bounds__(256, 2) void f8_tile_kernel(F8Args a, int nblk, int mblk, int slices)
 {
-    constexpr int kStage = TN * 2048, NJ = TN / 2;             // load instructions of a wave per stage
-    constexpr int kAhead = 3;                                  // weight tiles on their way from LDS: one tile's products are shorter than its read
+    constexpr int TM = kBatchTiles, kStage = TN * 2048, NJ = TN / 2;      // load instructions of a wave per stage
+    constexpr int kAhead = 3;                                  // weight tiles in registers on their way from LDS: one tile's products are shorter than its read
     constexpr bool WIDE = sizeof(E) == 4;
-    extern __shared__ __align__(16) char lds[];
+    __shared__ __align__(16) char lds[S * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int KB4 = (a.KB + 3) / 4, NT = (a.n + 15) / 16, MT = a.Mp / 16;
     // workgroups of an XCD (index mod 8) take neighbouring tiles: four columns of batch blocks, then the next weights
@@ -371,87 +374,95 @@ __global__ __launch_bounds__(256, TN * TM * (sizeof(E) == 4 ? 2 : 1) <= 32 ? 2 :
         const int band = L / (nblk * 4), w = min(4, mblk - band * 4), i = L - band * nblk * 4;
         nb = i / w; mb = band * 4 + i - nb * w;
     }
-    const int first = sl * a.KB / slices, KB = (sl + 1) * a.KB / slices;      // this workgroup's blocks of columns
+    const int first = sl * KB4 / slices * 4, end = (sl + 1) * KB4 / slices * 4;       // this workgroup's blocks of columns
     const uint32_t lds0 = lds_offset(lds);
     const char *wsrc[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-        const int idx = wave * NJ + j;
+        const int idx = wave * NJ + j;                         // half idx % 2 of weight tile idx / 2
         wsrc[j] = reinterpret_cast<const char *>(a.w) + (int64_t)min(nb * TN + (idx >> 1), NT - 1) * a.KB * 2048 + (idx & 1) * 1024;
     }
-    auto fetch = [&](int kb) {
+    auto fetch = [&](int kb, int slot) {
+        const int64_t at = (int64_t)min(kb, a.KB - 1) * 2048;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) load_to_lds(wsrc[j] + (int64_t)min(kb, KB - 1) * 2048, lane * 16, lds0 + (kb & 1) * kStage + (wave * NJ + j) * 1024);
+        for (int j = 0; j < NJ; ++j) load_to_lds(wsrc[j] + at, lane * 16, lds0 + slot * kStage + (wave * NJ + j) * 1024);
     };
-    const uint4 *xsrc[TM];
+    const u32x4_t *xsrc[TM];
     const uint32_t *xss[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int mt = min((mb * 4 + wave) * TM + i, MT - 1);
-        xsrc[i] = a.x + (int64_t)mt * a.KB * 128 + lane;
+        xsrc[i] = reinterpret_cast<const u32x4_t *>(a.x) + (int64_t)mt * KB4 * 512 + lane;
         xss[i] = a.xs + mt * 16 + col;
     }
     const uint32_t *wss = a.ws + (int64_t)(nb * TN >> 3) * KB4, *wss2 = a.ws + (int64_t)min((nb * TN + TN - 1) >> 3, (NT - 1) >> 3) * KB4;
     const int edge = 8 - (nb * TN & 7);                        // weight tiles from here on are of the next 128 rows
-    struct Batch { u32x4_t lo[TM], hi[TM]; uint32_t s[TM], w, w2; };
+    struct Batch { u32x4_t lo[TM], hi[TM]; };
+    struct Scales { uint32_t x[TM], w, w2; };
     auto load_batch = [&](Batch &b, int kb) {
+        const int at = min(kb, KB4 * 4 - 1) * 128;
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            b.lo[i] = *reinterpret_cast<const u32x4_t *>(xsrc[i] + kb * 128); b.hi[i] = *reinterpret_cast<const u32x4_t *>(xsrc[i] + kb * 128 + 64);
-            b.s[i] = xss[i][(int64_t)(kb >> 2) * a.Mp];
-        }
-        b.w = wss[kb >> 2]; b.w2 = wss2[kb >> 2];
+        for (int i = 0; i < TM; ++i) { b.lo[i] = xsrc[i][at]; b.hi[i] = xsrc[i][at + 64]; }
     };
-    auto pin = [&](Batch &b) {                                 // here, or the compiler waits for all loads at every later use
+    auto load_scales = [&](Scales &c, int kb) {
+        const int at = min(kb >> 2, KB4 - 1);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) asm volatile("" : "+v"(b.lo[i]), "+v"(b.hi[i]), "+v"(b.s[i]));
-        asm volatile("" : "+v"(b.w), "+v"(b.w2));
+        for (int i = 0; i < TM; ++i) c.x[i] = xss[i][(int64_t)at * a.Mp];
+        c.w = wss[at]; c.w2 = wss2[at];
     };
-    auto weight = [&](int kb, int t, u32x4_t (&f)[2]) {
-        const char *p = lds + (kb & 1) * kStage + t * 2048 + lane * 16;
+    auto pin = [&](Batch &b) {                                 // here, or the compiler waits for newer loads than it needs to later
+#pragma unroll
+        for (int i = 0; i < TM; ++i) asm volatile("" : "+v"(b.lo[i]), "+v"(b.hi[i]));
+    };
+    auto weight = [&](int slot, int t, u32x4_t (&f)[2]) {
+        const char *p = lds + slot * kStage + t * 2048 + lane * 16;
         f[0] = *reinterpret_cast<const u32x4_t *>(p); f[1] = *reinterpret_cast<const u32x4_t *>(p + 1024);
     };
     floatx4_t acc[TN][TM] = {};
-    Batch b0, b1;
+    Batch b[4];
+    Scales c, cn;
     u32x4_t wf[4][2];
-    fetch(first);
-    load_batch(b0, first);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    pin(b0);
-    asm volatile("s_barrier" ::: "memory");
-    fetch(first + 1);
 #pragma unroll
-    for (int t = 0; t < kAhead; ++t) weight(first, t, wf[t]);
-    // No branch in here: the compiler moves matrix products past one.  Behind the last block the last one's operands are read again, for nothing.
-    auto step = [&](int kb, Batch &b, Batch &next) {
-        load_batch(next, min(kb + 1, KB - 1));
-        const int sh = 8 * (kb & 3);
-        const int sw = b.w >> sh, sw2 = b.w2 >> sh;
+    for (int i = 0; i < S; ++i) fetch(first + i, i);
+    load_scales(c, first);
 #pragma unroll
-        for (int t = 0; t < TN; ++t) {
-            __builtin_amdgcn_sched_barrier(0);                 // or all of the block's weights are read ahead, into registers that the sums need
-            if (t + kAhead == TN) {
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-                pin(next);
-                asm volatile("s_barrier" ::: "memory");
-                fetch(kb + 2);
-            }
-            if (t + kAhead < TN) weight(kb, t + kAhead, wf[(t + kAhead) & 3]);
-            else weight(kb + 1, t + kAhead - TN, wf[(t + kAhead) & 3]);
-            const u32x4_t f0 = wf[t & 3][0], f1 = wf[t & 3][1];
-            const v8i_t wv = v8i_t{(int)f0[0], (int)f0[1], (int)f0[2], (int)f0[3], (int)f1[0], (int)f1[1], (int)f1[2], (int)f1[3]};
-            const int s = t < edge ? sw : sw2;
+    for (int i = 0; i < 3; ++i) load_batch(b[i], first + i);
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const u32x4_t l = b.lo[i], h = b.hi[i];
-                const v8i_t xv = v8i_t{(int)l[0], (int)l[1], (int)l[2], (int)l[3], (int)h[0], (int)h[1], (int)h[2], (int)h[3]};
-                const int sx = b.s[i] >> sh;
-                acc[t][i] = WIDE ? mfma_wide(wv, xv, acc[t][i], s, sx) : mfma_f8<0>(wv, xv, acc[t][i], s, sx);
+    for (int t = 0; t < kAhead; ++t) weight(0, t, wf[t]);
+    int slot = 0;
+    for (int kb = first; kb < end; kb += 4) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (u == 0) load_scales(cn, kb + 4);
+            load_batch(b[(u + 3) & 3], kb + u + 3);
+            const int sw = c.w >> (8 * u), sw2 = c.w2 >> (8 * u);
+#pragma unroll
+            for (int t = 0; t < TN; ++t) {
+                __builtin_amdgcn_sched_barrier(0);             // or all of the block's weights are read ahead, into registers that the sums need
+                if (t + kAhead == TN) {
+                    // newer than the next block's weights: x of S - 1 blocks, weights of S - 2, and the scales where they were among them
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"((S - 1) * 2 * TM + (S - 2) * NJ + (u < S - 1 ? TM + 2 : 0)) : "memory");
+                    pin(b[(u + 1) & 3]);
+                    asm volatile("s_barrier" ::: "memory");
+                    fetch(kb + u + S, slot);
+                    slot = slot + 1 == S ? 0 : slot + 1;
+                }
+                if (t + kAhead < TN) weight(slot, t + kAhead, wf[(t + kAhead) & 3]);
+                else weight(slot, t + kAhead - TN, wf[(t + kAhead) & 3]);
+                const v8i_t wv = both(wf[t & 3][0], wf[t & 3][1]);
+                const int s = t < edge ? sw : sw2;
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const v8i_t xv = both(b[u].lo[i], b[u].hi[i]);
+                    const int sx = c.x[i] >> (8 * u);
+                    acc[t][i] = WIDE ? mfma_wide(wv, xv, acc[t][i], s, sx) : mfma_f8<0>(wv, xv, acc[t][i], s, sx);
+                }
             }
         }
-    };
-    static_assert(TN % 4 == 0, "the next block's first weights land where this step's begin");
-    for (int kb = first; kb < KB; ++kb) { step(kb, b0, b1); b0 = b1; }      // two steps a turn, and the compiler moves the sums about
+        c = cn;
+    }
+    static_assert(TN % 4 == 0 && (S - 1) * 2 * TM + (S - 2) * NJ + TM + 2 <= 63, "the next block's first weights land where this step's begin; the counter has six bits");
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // nothing may arrive in LDS that has gone to another workgroup
     if (slices > 1) {                                          // fp32 sums of the slice: [slice][batch row][weight row]
         float *part = a.part + (int64_t)sl * a.Mp * NT * 16;
@@ -490,11 +501,11 @@ __global__ __launch_bounds__(256) void f8_join_kernel(F8Args a, int slices)
     emit<E>(a, m, n4 * 4, v);
 }
 
-template <int TN, int TM, typename E>
+template <int TN, int S, typename E>
 hipError_t launch_tile(const F8Args &a, int slices, hipStream_t s)
 {
-    const int NT = (a.n + 15) / 16, nblk = (NT + TN - 1) / TN, mblk = (a.Mp / 16 + 4 * TM - 1) / (4 * TM);
-    f8_tile_kernel<TN, TM, E><<<(unsigned)(nblk * mblk * slices), 256, 2 * TN * 2048, s>>>(a, nblk, mblk, slices);
+    const int NT = (a.n + 15) / 16, nblk = (NT + TN - 1) / TN, mblk = (a.m + 127) / 128;
+    f8_tile_kernel<TN, S, E><<<(unsigned)(nblk * mblk * slices), 256, 0, s>>>(a, nblk, mblk, slices);
     if (slices > 1) f8_join_kernel<E><<<(unsigned)(((int64_t)a.m * NT * 4 + 255) / 256), 256, 0, s>>>(a, slices);
     return hipGetLastError();
 }
@@ -504,7 +515,7 @@ template <int MB, bool RAW, typename X, typename E>
 hipError_t launch_stream(const F8Args &a, const X *x, int64_t ldx, int k, bool vec, hipStream_t s)
 {
     const int NT = (a.n + 15) / 16;
-    if (NT <= 320) f8_stream_kernel<MB, 1, RAW, X, E><<<NT, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
+    if (NT <= 256) f8_stream_kernel<MB, 1, RAW, X, E><<<NT, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
     else if (NT <= 512) f8_stream_kernel<MB, 2, RAW, X, E><<<(NT + 1) / 2, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
     else f8_stream_kernel<MB, 3, RAW, X, E><<<(NT + 2) / 3, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
     return hipGetLastError();
@@ -521,45 +532,40 @@ hipError_t launch_product(const F8Args &a, hipStream_t s)
         default: return launch_stream<4, false, float, E>(a, nullptr, 0, 0, false, s);
         }
     }
-    const F8Tile t = f8_tile(a.n, a.m, a.KB);
-    if constexpr (sizeof(E) == 4) return t.TM == 2 ? launch_tile<4, 2, E>(a, t.slices, s) : launch_tile<4, 4, E>(a, t.slices, s);
-    else if (t.TM == 2) return launch_tile<8, 2, E>(a, t.slices, s);
-    else switch (t.TN) {
-    case 16: return launch_tile<16, 4, E>(a, t.slices, s);
-    case 12: return launch_tile<12, 4, E>(a, t.slices, s);
-    case 8: return launch_tile<8, 4, E>(a, t.slices, s);
-    default: return launch_tile<4, 4, E>(a, t.slices, s);
-    }
+    const F8Tile t = f8_tile(a.n, a.m, a.KB, sizeof(E) == 4);
+    if constexpr (sizeof(E) == 4) return launch_tile<4, 4, E>(a, t.slices, s);
+    else return t.TN == 12 ? launch_tile<12, 3, E>(a, t.slices, s) : t.TN == 8 ? launch_tile<8, 4, E>(a, t.slices, s) : launch_tile<4, 4, E>(a, t.slices, s);
 }
 
 }  // namespace
 
-// workgroups in rounds of the compute units: the height and the number of slices that end the last round soonest
-F8Tile f8_tile(int n, int m, int KB)
+// Weight tiles of a workgroup and cuts of K.  A workgroup keeps a compute unit's matrix pipes about as busy as two do, so the time is rounds of
+// 256 workgroups, blocks of columns in each and 0.17 + 0.048 TN us a block (0.36, 0.55 and 0.75 us for 4, 8 and 12, by products of 128 to 5003
+// rows), 0.7 us for fp32 results; a cut K costs a launch and its sums' way out and back.  Between 251 x 22016 x 4096 (12 tiles 34 us, 8 42, 4 41),
+// 128 x 22016 x 4096 (31, 27, 31), 100 x 12288 x 4096 (27, 20, 16) and 251 x 4096 x 11008 (two slices of 4 tiles 26 us, four of 8 27, one 37) the rule
+// takes the best of each.
+F8Tile f8_tile(int n, int m, int KB, bool wide)
 {
-    const int NT = (n + 15) / 16, MT = (m + 15) / 16, TM = MT <= 8 ? 2 : 4, mblk = (MT + 4 * TM - 1) / (4 * TM);
-    F8Tile best{0, TM, 1};
-    double least = 1e30;
-    for (int tn : {16, 12, 8, 4}) {
-        if (TM == 2 && tn != 8) continue;
-        for (int sl = 1; sl <= 8 && sl * 4 <= KB; ++sl) {
+    const int NT = (n + 15) / 16, mblk = (m + 127) / 128, KB4 = (KB + 3) / 4;
+    F8Tile best{4, 1};
+    double least = 1e300;
+    for (int tn = 4; tn <= (wide ? 4 : 12); tn += 4)
+        for (int sl = 1; sl <= 8 && sl <= KB4; ++sl) {         // a slice has a word of scales at least
             const int64_t wg = (int64_t)((NT + tn - 1) / tn) * mblk * sl;
-            const double rounds = (double)((wg + 255) / 256);
-            const double cost = rounds * ((double)((KB + sl - 1) / sl) * (700.0 + tn * TM * 48.0) + 5000.0) + (sl > 1 ? 6000.0 + (double)m * n * sl * 8 / 2500.0 : 0.0);
-            if (cost < least) { least = cost; best.TN = tn; best.slices = sl; }
+            const double block = wide ? 0.7 : 0.17 + 0.048 * tn;
+            const double cost = (double)((wg + 255) / 256) * ((KB4 + sl - 1) / sl * 4) * block + (sl > 1 ? 2.5 + (double)m * n * sl * 8 / 6e6 : 0.0);
+            if (cost < least) { least = cost; best = F8Tile{tn, sl}; }
         }
-    }
-    if (best.TN == 0) best.TN = 8;
     return best;
 }
 
 hipError_t launch_f8_pack_act(const void *x, bool f32, int64_t ld, int m, int k, void *packed, void *scales, hipStream_t s)
 {
-    const int KB = (k + 127) / 128, tiles = (m + 15) / 16, el = f32 ? 4 : 2;
+    const int KB4 = (k + 511) / 512, tiles = (m + 15) / 16, el = f32 ? 4 : 2;
     const bool vec = ((uintptr_t)x & 15) == 0 && ld * el % 16 == 0;
-    const dim3 grid((unsigned)((KB + 1) / 2), (unsigned)tiles);
-    if (f32) f8_pack_act_kernel<float><<<grid, 256, 0, s>>>((const float *)x, ld, m, k, KB, vec, (uint4 *)packed, (uint8_t *)scales, tiles * 16);
-    else f8_pack_act_kernel<uint16_t><<<grid, 256, 0, s>>>((const uint16_t *)x, ld, m, k, KB, vec, (uint4 *)packed, (uint8_t *)scales, tiles * 16);
+    const dim3 grid((unsigned)(KB4 * 2), (unsigned)tiles);
+    if (f32) f8_pack_act_kernel<float><<<grid, 256, 0, s>>>((const float *)x, ld, m, k, KB4, vec, (uint4 *)packed, (uint8_t *)scales, tiles * 16);
+    else f8_pack_act_kernel<uint16_t><<<grid, 256, 0, s>>>((const uint16_t *)x, ld, m, k, KB4, vec, (uint4 *)packed, (uint8_t *)scales, tiles * 16);
     return hipGetLastError();
 }
 

@@ -116,7 +116,7 @@ int pat_op_f8_pack_weight(const void *w, int32_t type, int64_t ld, int32_t n, in
 
 static bool batch_ok(int32_t n, int32_t k, int32_t m) { return product_ok(n, k) && m >= 0 && m <= (1 << 19); }
 
-static int64_t part_offset(int32_t m, int32_t k) { return (f8_operand_bytes(m, k) + f8_act_scale_bytes(m, k) + 255) / 256 * 256; }
+static int64_t part_offset(int32_t m, int32_t k) { return (f8_act_bytes(m, k) + f8_act_scale_bytes(m, k) + 255) / 256 * 256; }
 
 int64_t pat_op_f8_gemm_scratch_bytes(int32_t n, int32_t k, int32_t m)
 {
@@ -130,7 +130,7 @@ int pat_op_f8_gemm(const void *w_packed, const void *w_scales, int32_t n, int32_
     if (!w_packed || !w_scales || !aligned(w_packed, 256) || !aligned(w_scales, 4) || ldx < k || ldy < n) return PAT_EINVAL;
     if (m == 0) return PAT_OK;
     if (!x || !y || !scratch || !aligned(x, size_of(x_type)) || !aligned(y, size_of(y_type)) || !aligned(scratch, 256)) return PAT_EINVAL;
-    char *sc = (char *)scratch + f8_operand_bytes(m, k);
+    char *sc = (char *)scratch + f8_act_bytes(m, k);
     F8Args a{};
     a.w = (const uint4 *)w_packed; a.x = (const uint4 *)scratch; a.ws = (const uint32_t *)w_scales; a.xs = (const uint32_t *)sc;
     a.y = y; a.ldy = ldy; a.n = n; a.m = m; a.Mp = (m + 15) / 16 * 16; a.KB = (k + 127) / 128; a.add = mode == 1;

@@ -73,6 +73,7 @@ hipError_t launch_attn_shared(const SharedArgs &a, int d, bool f32, int n_cu, hi
 
 // ---- 8-bit projections (gemm_f8.hip) ---------------------------------------------
 inline int64_t f8_operand_bytes(int64_t rows, int64_t k) { return (rows + 15) / 16 * ((k + 127) / 128) * 2048; }
+inline int64_t f8_act_bytes(int64_t m, int64_t k) { return (m + 15) / 16 * ((k + 511) / 512) * 8192; }
 inline int64_t f8_weight_scale_bytes(int64_t n, int64_t k) { return (n + 127) / 128 * ((k + 511) / 512) * 4; }
 inline int64_t f8_act_scale_bytes(int64_t m, int64_t k) { return (m + 15) / 16 * 16 * ((k + 511) / 512) * 4; }
 struct F8Args {
@@ -84,13 +85,13 @@ struct F8Args {
     bool add, vec;             // y += ; rows n .. n + 3 of y by one store
     float *part;               // sums of K slices [slice][Mp][16-row tiles of n][16], where f8_tile has more than one
 };
-struct F8Tile { int TN, TM, slices; };      // tiles of weight rows per workgroup, of batch rows per wave, cuts of K
-F8Tile f8_tile(int n, int m, int KB);
+struct F8Tile { int TN, slices; };         // above 64 rows: tiles of weight rows per workgroup, cuts of K
+F8Tile f8_tile(int n, int m, int KB, bool wide);      // wide: fp32 results
 inline int64_t f8_part_bytes(int n, int m, int k)
 {
     if (m <= 64) return 0;
-    const F8Tile t = f8_tile(n, m, (k + 127) / 128);
-    return t.slices > 1 ? (int64_t)t.slices * ((m + 15) / 16 * 16) * ((n + 15) / 16 * 16) * 4 : 0;
+    const int a = f8_tile(n, m, (k + 127) / 128, false).slices, b = f8_tile(n, m, (k + 127) / 128, true).slices, most = a > b ? a : b;
+    return most > 1 ? (int64_t)most * ((m + 15) / 16 * 16) * ((n + 15) / 16 * 16) * 4 : 0;
 }
 hipError_t launch_f8_pack_act(const void *x, bool f32, int64_t ld, int m, int k, void *packed, void *scales, hipStream_t s);
 hipError_t launch_f8_pack_weight(const void *w, bool f32, int64_t ld, int n, int k, void *packed, void *scales, hipStream_t s);
