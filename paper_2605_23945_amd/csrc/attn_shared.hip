@@ -74,9 +74,9 @@ __device__ __forceinline__ int find(const int32_t *off, int n, int x)
 __device__ __forceinline__ int up(int64_t v, int to) { return (int)((v + to - 1) / to * to); }
 
 // One workgroup.  A group shares its prefix if at least two of its sequences reach its end; others, and sequences shorter
-// than their group's prefix, are read whole through their own rows.  Chunks: a workgroup's work is measured in keys per
-// wave, all of it shared out evenly over the resident workgroups gives the chunk, within [32, 256] keys per wave (below, an
-// item's fixed cost is most of it; above, nothing is gained), and never so short that the parts pass what shared_parts() holds.
+// than their group's prefix, are read whole through their own rows.  Chunks: an item costs about two and a half tiles of 32 keys
+// per wave beside its own, and two workgroups are resident on a compute unit; of 1 to 8 tiles per wave the number is taken that makes rounds times an item's
+// cost least, with half a chunk for every row block's last one, and never one so short that the parts pass what shared_parts() holds.
 __global__ __launch_bounds__(kPlan) void attn_plan_kernel(SharedPlanArgs a)
 {
     __shared__ int32_t gcnt[kSharedMaxSeqs], gfirst[kSharedMaxSeqs], grec[kSharedMaxSeqs + 1], gpart[kSharedMaxSeqs + 1], srec[kSharedMaxSeqs + 1];
@@ -112,24 +112,32 @@ __global__ __launch_bounds__(kPlan) void attn_plan_kernel(SharedPlanArgs a)
     }
     __syncthreads();
     // work: row blocks times keys of the groups and of the sequences, and parts times keys
-    int64_t wp = 0, ws = 0, pp = 0;
+    int64_t wp = 0, ws = 0, pp = 0, nb = 0, ns = 0;            // and their row blocks
     int from[2];                                               // first key that sequence s reads by itself
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         in[i] = in[i] && gcnt[grp[i]] >= 2;
         from[i] = in[i] ? a.shared_len[grp[i]] : 0;
         ws += (int64_t)GB * (len[i] - from[i]);
+        ns += len[i] > from[i] ? GB : 0;
     }
     for (int g = tid; g < ng; g += kPlan)
         if (gcnt[g] >= 2) {
             const int members = a.group_start[g + 1] - a.group_start[g];
+            nb += (members * G + kSharedRows - 1) / kSharedRows;
             wp += (int64_t)((members * G + kSharedRows - 1) / kSharedRows) * a.shared_len[g];
             pp += (int64_t)members * a.shared_len[g];
         }
-    wp = block_sum(wp, tmp); ws = block_sum(ws, tmp); pp = block_sum(pp, tmp);
+    wp = block_sum(wp, tmp); ws = block_sum(ws, tmp); pp = block_sum(pp, tmp); nb = block_sum(nb, tmp); ns = block_sum(ns, tmp);
     const bool solo = a.hkv % kW == 0;
-    const int64_t per = ((wp + ws) * a.hkv + kW * 2 * a.n_cu - 1) / (kW * 2 * a.n_cu);
-    const int c = (int)min((int64_t)256, max((int64_t)32, (per + 31) / 32 * 32));
+    int c = 32;
+    float least = INFINITY;
+    for (int t = 1; t <= 8; ++t) {                             // tiles of a wave
+        const float keys = (float)(32 * t), own = solo ? (float)ws / keys : (float)ws / (keys * kW);
+        const float items = (float)a.hkv * ((float)wp / (keys * kW) + 0.5f * (float)nb) + (float)(solo ? a.hkv / kW : a.hkv) * (own + 0.5f * (float)ns);
+        const float rounds = items / (float)(2 * a.n_cu), cost = (rounds <= 1.f ? 1.f : rounds + 0.3f) * (2.5f + (float)t);
+        if (cost < least) { least = cost; c = 32 * t; }
+    }
     const int64_t room = 2 * (int64_t)n + 512;                 // chunks beyond the first of each group's members, or sequence
     const int CP = max(c * kW, up(pp / room + 1, kTile * kW)), CS = max(solo ? c : c * kW, up(ws / room + 1, kTile));
 
@@ -166,9 +174,13 @@ __global__ __launch_bounds__(kPlan) void attn_plan_kernel(SharedPlanArgs a)
         q.s0 = parts + srec[s]; q.sn = srec[s + 1] - srec[s];
         seqs[s] = q;
     }
-    for (int r = tid; r < np; r += kPlan) {                    // a chunk's row blocks are neighbours: they read the same keys
+    // A chunk's row blocks read the same keys: they come D records apart, so that their workgroups, hkv to a record and dealt to the eight XCDs in
+    // turn, share an XCD's L2.
+    const int D = 8 / ((a.hkv & 7) == 0 ? 8 : a.hkv & -a.hkv);
+    for (int r = tid; r < np; r += kPlan) {
         const int g = find(grec, ng, r), k = r - grec[g], lo = a.group_start[g], members = a.group_start[g + 1] - lo;
-        const int nb = (members * G + kSharedRows - 1) / kSharedRows, ch = k / nb, rb = k - ch * nb;
+        const int nb = (members * G + kSharedRows - 1) / kSharedRows, nc = (a.shared_len[g] + CP - 1) / CP;
+        const int blk = k / (D * nb), rem = k - blk * D * nb, w = min(D, nc - blk * D), rb = rem / w, ch = blk * D + rem - rb * w;
         SharedRecord e{};
         e.seq0 = lo; e.r0 = rb * kSharedRows; e.rows = min(kSharedRows, members * G - e.r0);
         e.table_row = gfirst[g];
@@ -242,18 +254,41 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
         if (wrong) page = 0;
         bad |= __any(wrong) != 0;
     };
-    auto request = [&](const char *pool, int i, uint32_t at) {
-        const int key0 = tb + (i * ws + w0) * kTile;
+    // Where the halves of the wave's tile i lie in both pools, and the lane's place in them: 16 keys of a page are consecutive, so inside the
+    // record's keys a load's address is a sum of one scalar and one of NI / 2 constants.
+    uint32_t place[NI / 2];
 #pragma unroll
-        for (int u = 0; u < NI; ++u) {
-            const int half = u * KPI / 16, key = u * KPI + lane / PC, src = max(min(key0 + key, last), e.t0);      // keys outside repeat a valid one: finite values, weight 0
-            const uint32_t off = (uint32_t)((src & (P - 1)) * (D * 2)) + (uint32_t)(((lane % PC) ^ (key & (PC - 1))) * 16);
-            const char *base = pool + __builtin_amdgcn_readlane(page, 2 * (i & 31) + half) * page_bytes;
-            if (once) load_to_lds_stream(base, off, at + u * 1024);
-            else load_to_lds(base, off, at + u * 1024);
+    for (int u = 0; u < NI / 2; ++u) {
+        const int key = u * KPI + lane / PC;
+        place[u] = (uint32_t)(key * (D * 2) + ((lane % PC) ^ (key & (PC - 1))) * 16);
+    }
+    struct Halves { int64_t at[2]; bool inside; int key0; };
+    auto halves = [&](int i) {
+        Halves t;
+        t.key0 = tb + (i * ws + w0) * kTile;
+        t.inside = t.key0 >= e.t0 && t.key0 + kTile - 1 <= last;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            t.at[j] = __builtin_amdgcn_readlane(page, 2 * (i & 31) + j) * page_bytes + (int64_t)((t.inside ? (t.key0 + j * 16) & (P - 1) : 0) * (D * 2));
+        return t;
+    };
+    auto request = [&](const char *pool, const Halves &t, uint32_t at) {
+        if (t.inside && once) {
+#pragma unroll
+            for (int u = 0; u < NI; ++u) load_to_lds_stream(pool + t.at[u / (NI / 2)], place[u % (NI / 2)], at + u * 1024);
+        } else if (t.inside) {
+#pragma unroll
+            for (int u = 0; u < NI; ++u) load_to_lds(pool + t.at[u / (NI / 2)], place[u % (NI / 2)], at + u * 1024);
+        } else {
+#pragma unroll
+            for (int u = 0; u < NI; ++u) {                     // keys outside repeat a valid one: finite values, weight 0
+                const int key = u * KPI + lane / PC, src = max(min(t.key0 + key, last), e.t0);
+                load_to_lds(pool + t.at[u / (NI / 2)], (uint32_t)((src & (P - 1)) * (D * 2) + ((lane % PC) ^ (key & (PC - 1))) * 16), at + u * 1024);
+            }
         }
     };
-    if (n > 0) { look_up(0); request(kpool, 0, to); request(vpool, 0, to + kHalf); }
+    Halves now{};
+    if (n > 0) { look_up(0); now = halves(0); request(kpool, now, to); request(vpool, now, to + kHalf); }
 
     u32x4_t q[RT][KST][QT];
 #pragma unroll
@@ -285,7 +320,8 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // read: the place can be requested anew
         if (i + 1 < n) {
             if (((i + 1) & 31) == 0) look_up(i + 1);
-            request(kpool, i + 1, to);
+            now = halves(i + 1);
+            request(kpool, now, to);
         }
         u32x4_t ph[RT], pm[RT], pl[RT];
 #pragma unroll
@@ -342,7 +378,7 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
             vf[f] = u32x4_t{va.x, va.y, vb.x, vb.y};
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (i + 1 < n) request(vpool, i + 1, to + kHalf);
+        if (i + 1 < n) request(vpool, now, to + kHalf);
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
 #pragma unroll
@@ -433,10 +469,15 @@ __global__ __launch_bounds__(kW * 64, 2) void attn_shared_kernel(SharedArgs a)
     if (!made_for(head, a)) return;
     const int np = head->n_prefix, no = head->n_own, solo = head->solo, hkv = a.hkv, per = solo ? hkv / kW : hkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t first_own = (int64_t)np * hkv, items = first_own + (int64_t)no * per;
+    // fp32 queries, three terms each, leave registers for one row tile of 16: a record's second tile is an item of its own
+    const int halves = F32 ? 2 : 1, own_halves = F32 && a.hq / hkv > 16 ? 2 : 1;
+    const int64_t first_own = (int64_t)np * hkv * halves, items = first_own + (int64_t)no * per * own_halves;
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
         const bool prefix = it < first_own;
-        const uint32_t x = (uint32_t)(prefix ? it : it - first_own), div = prefix ? hkv : per, ri = x / div;
+        uint32_t x = (uint32_t)(prefix ? it : it - first_own);
+        const uint32_t div = prefix ? hkv : per, of = (prefix ? np : no) * div, half = F32 && x >= of ? 1 : 0;
+        x -= half * of;
+        const uint32_t ri = x / div;
         const bool together = prefix || !solo;
         const int h = (int)(x - ri * div) * (together ? 1 : kW) + (together ? 0 : wave);
         const SharedRecord *rp = recs + (prefix ? ri : np + ri);
@@ -444,7 +485,13 @@ __global__ __launch_bounds__(kW * 64, 2) void attn_shared_kernel(SharedArgs a)
         e.seq0 = __builtin_amdgcn_readfirstlane(rp->seq0); e.r0 = __builtin_amdgcn_readfirstlane(rp->r0); e.rows = __builtin_amdgcn_readfirstlane(rp->rows);
         e.table_row = __builtin_amdgcn_readfirstlane(rp->table_row); e.t0 = __builtin_amdgcn_readfirstlane(rp->t0); e.cnt = __builtin_amdgcn_readfirstlane(rp->cnt);
         e.part0 = __builtin_amdgcn_readfirstlane(rp->part0);
-        if (e.rows <= 16) item<D, 1, F32>(a, e, h, together, !prefix, lds, wml);
+        if (F32) {
+            e.r0 += half * 16;
+            e.rows = min(16, e.rows - (int)half * 16);
+            if (e.rows <= 0) continue;
+        }
+        if constexpr (F32) item<D, 1, F32>(a, e, h, together, !prefix, lds, wml);
+        else if (e.rows <= 16) item<D, 1, F32>(a, e, h, together, !prefix, lds, wml);
         else item<D, 2, F32>(a, e, h, together, !prefix, lds, wml);
     }
 }
@@ -458,7 +505,7 @@ __device__ __forceinline__ void put(uint16_t *p, float v) { *p = f32_to_bf16(v);
 template <int D, typename E>
 __global__ __launch_bounds__(256) void attn_join_kernel(SharedArgs a)
 {
-    constexpr int N = D / 64;
+    constexpr int N = D / 64, kTogether = 8;
     const int lane = threadIdx.x & 63;
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= (int64_t)a.n_seqs * a.hq) return;
@@ -487,11 +534,22 @@ __global__ __launch_bounds__(256) void attn_join_kernel(SharedArgs a)
             l = fmaf(ml.y, w, l);
         }
         const int m = min(64, n - i0);
-        for (int i = 0; i < m; ++i) {
-            const float wi = __shfl(w, i, 64);
-            const float *p = a.part_acc + part(i0 + i) * D + lane;
+        for (int i = 0; i < m; i += kTogether) {               // loads of several parts on their way; one behind the last repeats it with weight 0
+            float v[kTogether][N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) acc[k] = fmaf(p[k * 64], wi, acc[k]);
+            for (int j = 0; j < kTogether; ++j) {
+                const float *p = a.part_acc + part(i0 + min(i + j, m - 1)) * D + lane;
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[j][k] = p[k * 64];
+            }
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) {
+                const float wj = __shfl(w, i + j, 64);
+                if (i + j < m) {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) acc[k] = fmaf(v[j][k], wj, acc[k]);
+                }
+            }
         }
     }
     l = wave_sum(l);

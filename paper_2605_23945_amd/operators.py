@@ -27,12 +27,12 @@ def _on(t, *others):
 
 def _call(dev, name, *args):
     """The library's call with its device the current one, on that device's current stream."""
-    fn = getattr(load_library(), name)
-    if torch.cuda.current_device() != dev.index:
-        with torch.cuda.device(dev):
-            rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    fn, at = getattr(load_library(), name), dev.index
+    if torch.cuda.current_device() != at:
+        with torch.cuda.device(at):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(at))
     else:
-        rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(at))
     if rc:
         raise PatError(rc, name)
 
