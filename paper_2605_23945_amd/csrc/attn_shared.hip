@@ -206,6 +206,16 @@ __global__ __launch_bounds__(kPlan) void attn_plan_kernel(SharedPlanArgs a)
 template <int N>
 __device__ __forceinline__ void wait_newer() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }     // all but the N newest loads have arrived
 
+// the largest of the four lanes of a column (lanes i, i + 16, i + 32, i + 48), in all of them: by exchanges between lane rows, without a way through LDS
+__device__ __forceinline__ float column_max(float v)
+{
+    const uint32_t b = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    const float m = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
+
 template <bool F32> struct QTerms { static constexpr int n = F32 ? 3 : 1, p = F32 ? 3 : 2; };
 
 // eight consecutive features of a query row as operand terms
@@ -287,9 +297,7 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
             }
         }
     };
-    Halves now{};
-    if (n > 0) { look_up(0); now = halves(0); request(kpool, now, to); request(vpool, now, to + kHalf); }
-
+    // q and the pages arrive before the stream begins: a wait left for the loop would be one for every load under way
     u32x4_t q[RT][KST][QT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -298,6 +306,15 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
 #pragma unroll
         for (int ks = 0; ks < KST; ++ks) load_q(p + ks * 32, q[t][ks]);
     }
+    Halves now{};
+    look_up(0);
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int ks = 0; ks < KST; ++ks)
+#pragma unroll
+            for (int x = 0; x < QT; ++x) asm volatile("" : "+v"(q[t][ks][x]));
+    if (n > 0) { now = halves(0); request(kpool, now, to); request(vpool, now, to + kHalf); }
     const float scale = rsqrtf((float)D) * 1.44269504f;        // scores in units of log2: p is one exp2 instruction
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -351,8 +368,7 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
             float mt = p[0];
 #pragma unroll
             for (int j = 1; j < 8; ++j) mt = fmaxf(mt, p[j]);
-            mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
-            mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+            mt = column_max(mt);
             const float Mn = fmaxf(M[t], mt * scale);
             if (__any(Mn > M[t])) {                            // some row of the tile has a new maximum
                 const float corr = M[t] == Mn ? 1.f : __builtin_amdgcn_exp2f(M[t] - Mn);     // exp2(-inf) = 0 on the wave's first keys
@@ -501,13 +517,16 @@ __global__ __launch_bounds__(kW * 64, 2) void attn_shared_kernel(SharedArgs a)
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(uint16_t *p, float v) { *p = f32_to_bf16(v); }
 
-// One wave per (sequence, query head): lane i holds features i and, of 128, i + 64; parts in order, the prefix's first.
-template <int D, typename E>
-__global__ __launch_bounds__(256) void attn_join_kernel(SharedArgs a)
+// W waves per (sequence, query head), wave w the parts w, w + W, ..: lane i holds features i and, of 128, i + 64.  Of the waves' sums, met in LDS, the
+// first makes the result, in their order.
+template <int D, int W, typename E>
+__global__ __launch_bounds__(W > 4 ? W * 64 : 256) void attn_join_kernel(SharedArgs a)
 {
-    constexpr int N = D / 64, kTogether = 8;
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int N = D / 64, kTogether = 8, kRows = W > 4 ? 1 : 4 / W;
+    static_assert(W == 1 || W > 4, "rows of a workgroup");
+    __shared__ float red[W][N + 1][W > 1 ? 64 : 1];
+    const int lane = threadIdx.x & 63, wave = W > 1 ? (int)(threadIdx.x >> 6) : 0;
+    const int64_t row = (int64_t)blockIdx.x * kRows + (W > 1 ? 0 : threadIdx.x >> 6);
     if (row >= (int64_t)a.n_seqs * a.hq) return;
     const int s = (int)(row / a.hq), hd = (int)(row - (int64_t)s * a.hq);
     const SharedHeader *head = reinterpret_cast<const SharedHeader *>(a.plan);
@@ -518,7 +537,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(SharedArgs a)
     if (q.bad || n == 0) {                                     // no keys: zero; a length that makes no sense: no number
         const float v = q.bad ? NAN : 0.f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) put(out + i * 64, v);
+        for (int i = 0; i < N; ++i)
+            if (wave == 0) put(out + i * 64, v);
         return;
     }
     auto part = [&](int i) { return (int64_t)(i < q.pn ? q.p0 + i * q.p_step : q.s0 + i - q.pn) * a.hq + hd; };
@@ -526,19 +546,19 @@ __global__ __launch_bounds__(256) void attn_join_kernel(SharedArgs a)
     for (int i = lane; i < n; i += 64) M = fmaxf(M, a.part_ml[part(i) * 2]);
     M = wave_max(M);
     float acc[N] = {}, l = 0.f;
-    for (int i0 = 0; i0 < n; i0 += 64) {
+    for (int i0 = wave; i0 < n; i0 += 64 * W) {                // lane j: weight of the wave's j-th part from here
         float w = 0.f;
-        if (i0 + lane < n) {
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + part(i0 + lane) * 2);
+        if (i0 + lane * W < n) {
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + part(i0 + lane * W) * 2);
             w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
             l = fmaf(ml.y, w, l);
         }
-        const int m = min(64, n - i0);
-        for (int i = 0; i < m; i += kTogether) {               // loads of several parts on their way; one behind the last repeats it with weight 0
+        const int m = min(64, (n - i0 + W - 1) / W);
+        for (int i = 0; i < m; i += kTogether) {               // loads of several parts on their way; one behind the last repeats it and is left out
             float v[kTogether][N];
 #pragma unroll
             for (int j = 0; j < kTogether; ++j) {
-                const float *p = a.part_acc + part(i0 + min(i + j, m - 1)) * D + lane;
+                const float *p = a.part_acc + part(i0 + min(i + j, m - 1) * W) * D + lane;
 #pragma unroll
                 for (int k = 0; k < N; ++k) v[j][k] = p[k * 64];
             }
@@ -553,6 +573,18 @@ __global__ __launch_bounds__(256) void attn_join_kernel(SharedArgs a)
         }
     }
     l = wave_sum(l);
+    if constexpr (W > 1) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) red[wave][k][lane] = acc[k];
+        red[wave][N][lane] = l;
+        __syncthreads();
+        if (wave) return;
+        for (int w = 1; w < W; ++w) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) acc[k] += red[w][k][lane];
+            l += red[w][N][lane];
+        }
+    }
     const float inv = 1.0f / l;
 #pragma unroll
     for (int k = 0; k < N; ++k) put(out + k * 64, acc[k] * inv);
@@ -568,7 +600,10 @@ hipError_t launch_shared(const SharedArgs &a, int n_cu, hipStream_t s)
     attn_shared_kernel<D, F32><<<grid, kW * 64, kW * kTile * D * 4, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    attn_join_kernel<D, E><<<(unsigned)(((int64_t)a.n_seqs * a.hq + 3) / 4), 256, 0, s>>>(a);
+    // few rows may have many parts each (32 rows of 133 parts: 17 us by a wave alone), many rows have few
+    const int64_t rows = (int64_t)a.n_seqs * a.hq;
+    if (rows <= 512) attn_join_kernel<D, 8, E><<<(unsigned)rows, 512, 0, s>>>(a);
+    else attn_join_kernel<D, 1, E><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
