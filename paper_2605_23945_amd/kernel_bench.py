@@ -1,13 +1,16 @@
 """Micro-benchmark of the weight-streaming projection kernels on the shapes of a configuration.
 
     python -m paper_2605_23945_amd.kernel_bench [--config 7b_tp1] [--batch 1,16,32,64,256] [--iters 30]
-                                                 [--only gateup,down,...,barrier] [--copy-gib 1]
+                                                 [--only gateup,down,...,barrier,append,attend,f8] [--copy-gib 1]
 
 Each projection is run on 6 distinct weight copies in rotation (more than the 256 MB
 memory-side cache holds), timed with events on the launch stream.  `--copy-gib` first runs a
 plain device-to-device copy of known size: under `rocprofv3 --pmc FETCH_SIZE` / `WRITE_SIZE` its
 counters calibrate the unit of the projection kernels' counters.  `--only barrier` times the device-wide barrier
 of the fused layer kernel instead (pat_op_barrier_probe) among 32, 64, 128 and 256 resident workgroups.
+`--only append,attend,f8` times the operators of group rollouts on the configuration's shapes: rotation and append of a step's
+rows, attention of the batch as groups of eight answers to prompts of `--prefix` tokens with `--suffix` of their own, and the projections on
+8-bit weights.
 """
 from __future__ import annotations
 
@@ -17,6 +20,61 @@ import os
 import sys
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+
+def _us(run, iters):
+    """Mean microseconds of a call, by events around `iters` of them."""
+    import torch
+    for i in range(6):
+        run(i)
+    torch.cuda.synchronize()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    e0.record()
+    for i in range(iters):
+        run(i)
+    e1.record()
+    torch.cuda.synchronize()
+    return e0.elapsed_time(e1) * 1e3 / iters
+
+
+def operators(s, kinds, batches, shapes, args, dev="cuda:0"):
+    """The operators of include/pat_operators.h on shard `s`."""
+    import torch
+    import paper_2605_23945_amd as pat
+    bf = torch.bfloat16
+    i32 = lambda a: torch.as_tensor(a, dtype=torch.int32, device=dev)
+    randn = lambda *shape: torch.randn(*shape, device=dev, dtype=bf)
+    hq, hkv, d, P = s.hq, s.hkv, s.head_dim, 64
+    for b in batches:
+        if "append" in kinds or "attend" in kinds:
+            members = min(8, b)
+            start = list(range(0, b, members)) + [b]
+            whole, own = args.prefix // P, -(-(args.prefix % P + args.suffix) // P)
+            n_pages = (len(start) - 1) * whole + b * own
+            order, table, at = torch.randperm(n_pages).tolist(), [], (len(start) - 1) * whole
+            for i in range(b):
+                g = i // members
+                table.append(order[g * whole:(g + 1) * whole] + order[at:at + own])
+                at += own
+            table, length = i32(table), args.prefix + args.suffix
+            pools = [[randn(n_pages, hkv, P, d) for _ in range(2)] for _ in range(2)]
+        if "append" in kinds:
+            cs, qkv, q = pat.pat_op_rope_table(length, d, s.model.rope_base, dev), randn(b, (hq + 2 * hkv) * d), randn(b, hq, d)
+            seq, pos = i32(range(b)), i32([length - 1] * b)
+            us = _us(lambda i: pat.pat_op_kv_append(qkv, seq, pos, cs, *pools[i % 2], table, q), args.iters)
+            print(f"append   B={b:4d} heads {hq}+{hkv}+{hkv} x {d}  {us:8.1f} us", flush=True)
+        if "attend" in kinds:
+            q, out = randn(b, hq, d), randn(b, hq, d)
+            plan = pat.pat_op_attn_plan(i32([length] * b), i32(start), i32([args.prefix] * (len(start) - 1)), length, hq, hkv, d)
+            us = _us(lambda i: pat.pat_op_attn_shared(q, *pools[i % 2], table, plan, out), args.iters)
+            nbytes = ((len(start) - 1) * args.prefix + b * args.suffix) * hkv * d * 4
+            print(f"attend   B={b:4d} groups of {members}, {args.prefix} + {args.suffix} tokens  {us:8.1f} us  {nbytes} B  {nbytes / us / 1e6:6.2f} TB/s", flush=True)
+        if "f8" in kinds:
+            for name, (n, k, _) in shapes.items():
+                ws = [pat.pat_op_f8_pack_weight(randn(n, k)) for _ in range(max(1, args.copies))]
+                x, y = randn(b, k), randn(b, n)
+                us = _us(lambda i: pat.pat_op_f8_gemm(*ws[i % len(ws)], n, x, y), args.iters)
+                print(f"f8 {name:8s} N={n:6d} K={k:6d} B={b:4d}  {us:8.1f} us  weights {n * k} B  {n * k / us / 1e6:6.2f} TB/s  {2 * n * k * b / us / 1e6:7.1f} TFLOP/s", flush=True)
 
 
 def main():
@@ -31,6 +89,8 @@ def main():
     ap.add_argument("--only", default="")
     ap.add_argument("--copy-gib", type=float, default=0.0)
     ap.add_argument("--copies", type=int, default=6, help="distinct weight copies used in rotation (1 = cache-resident if it fits)")
+    ap.add_argument("--prefix", type=int, default=1024, help="shared tokens of a group (attend)")
+    ap.add_argument("--suffix", type=int, default=512, help="own tokens of an answer (attend)")
     args = ap.parse_args()
     lib = pat.load_library()
     dev = "cuda:0"
@@ -57,6 +117,12 @@ def main():
             us = [pat.pat_op_barrier_probe(n_wg, iters=500) for _ in range(3)]
             print(f"barrier  workgroups={n_wg:4d}  {min(us):6.2f} us per barrier (best of 3 x 500; others {sorted(us)[1]:.2f}, {max(us):.2f})", flush=True)
         only = [x for x in only if x != "barrier"]
+        if not only:
+            return
+    kinds = [x for x in only if x in ("append", "attend", "f8")]
+    if kinds:
+        operators(s, kinds, [int(x) for x in args.batch.split(",")], shapes, args, dev)
+        only = [x for x in only if x not in kinds]
         if not only:
             return
     ncopy = max(1, args.copies)

@@ -16,12 +16,13 @@ def _need(ok, what):
         raise PatError(PAT_EINVAL, what)
 
 
-def _on(t, *others):
+def _one_device(t, *others):
     """The device of all these tensors (None: left out)."""
     dev = t.device
-    _need(dev.type == "cuda", "tensors on the GPU are needed")
+    ok = dev.type == "cuda"
     for o in others:
-        _need(o is None or o.device == dev, "tensors on one device are needed")
+        ok = ok and (o is None or o.device == dev)
+    _need(ok, "tensors on one GPU are needed")
     return dev
 
 
@@ -30,35 +31,39 @@ def _call(dev, name, *args):
     fn, at = getattr(load_library(), name), dev.index
     if torch.cuda.current_device() != at:
         with torch.cuda.device(at):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(at))
+            rc = fn(*args, torch.cuda.current_stream(at).cuda_stream)
     else:
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(at))
+        rc = fn(*args, torch.cuda.current_stream(at).cuda_stream)
     if rc:
         raise PatError(rc, name)
 
 
 def _cache(k, v):
     """[n_pages, heads, tokens of a page, features] of the two pools."""
-    _need(k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.dim() == 4 and k.shape == v.shape and k.is_contiguous() and v.is_contiguous(),
+    shape = k.shape
+    _need(k.dtype is torch.bfloat16 and v.dtype is torch.bfloat16 and len(shape) == 4 and shape == v.shape and k.is_contiguous() and v.is_contiguous(),
           "k and v pools: contiguous bf16 [n_pages, n_kv_heads, page_tokens, head_dim]")
-    return k.shape
+    return shape
 
 
 def _table(t):
-    _need(t.dtype == torch.int32 and t.dim() == 2 and t.is_contiguous(), "page_table: contiguous int32 [sequences, max_pages]")
-    return t.shape
+    shape = t.shape
+    _need(t.dtype is torch.int32 and len(shape) == 2 and t.is_contiguous(), "page_table: contiguous int32 [sequences, max_pages]")
+    return shape
 
 
 def _list(t, n, what):
-    _need(t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.shape[0] == n, f"{what}: contiguous int32 [{n}]")
+    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous():
+        _need(False, f"{what}: contiguous int32 [{n}]")
     return t.data_ptr()
 
 
 def _rows(t, heads, d, what):
     """Elements from row to row of [rows, heads, d] whose rows are dense."""
-    _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == d and t.dtype in _TYPE, f"{what}: fp32 or bf16 [rows, {heads}, {d}]")
-    _need(t.stride(2) == 1 and (heads == 1 or t.stride(1) == d), f"{what}: its rows have to be dense")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * d)
+    rows, strides = t.shape[0], t.stride()
+    if t.shape != (rows, heads, d) or t.dtype not in _TYPE or strides[2] != 1 or (heads > 1 and strides[1] != d):
+        _need(False, f"{what}: fp32 or bf16 [rows, {heads}, {d}], rows dense")
+    return strides[0] if rows > 1 else heads * d
 
 
 def pat_op_rope_table(n_pos, head_dim, base=10000.0, device="cuda:0"):
@@ -74,20 +79,21 @@ def pat_op_kv_append(qkv, seq, pos, cos_sin, k_pages, v_pages, page_table, q_out
     pages of sequence seq[i] at position pos[i] (both int32 [rows]); seq[i] < 0 is a row of padding.  skipped: NULL or int32 [1], raised by
     the rows that name no place of the cache.  Returns q_out."""
     n_pages, hkv, P, d = _cache(k_pages, v_pages)
-    dev = _on(qkv, seq, pos, cos_sin, k_pages, v_pages, page_table, q_out, gq, gk, skipped)
+    dev = _one_device(qkv, seq, pos, cos_sin, k_pages, v_pages, page_table, q_out, gq, gk, skipped)
     n_seqs, max_pages = _table(page_table)
     _need(qkv.dim() == 2 and qkv.dtype in _TYPE and qkv.stride(1) == 1 and q_out.dim() == 3 and q_out.dtype == qkv.dtype and q_out.shape[0] == qkv.shape[0],
           "qkv [rows, (hq + 2 hkv) d] and q_out [rows, hq, d]: fp32 or bf16 of one type, rows dense")
-    rows, hq = qkv.shape[0], q_out.shape[1]
-    _need(qkv.shape[1] == (hq + 2 * hkv) * d, f"qkv: {(hq + 2 * hkv) * d} features a row for {hq} q and {hkv} k and v heads, not {qkv.shape[1]}")
-    _need(cos_sin.dtype == torch.float32 and cos_sin.is_contiguous() and cos_sin.dim() == 3 and tuple(cos_sin.shape[1:]) == (d // 2, 2), "cos_sin: contiguous fp32 [positions, d / 2, 2]")
+    (rows, width), hq, n_pos = qkv.shape, q_out.shape[1], cos_sin.shape[0]
+    if width != (hq + 2 * hkv) * d:
+        _need(False, f"qkv: {(hq + 2 * hkv) * d} features a row for {hq} q and {hkv} k and v heads, not {width}")
+    _need(cos_sin.dtype is torch.float32 and cos_sin.is_contiguous() and cos_sin.shape == (n_pos, d // 2, 2), "cos_sin: contiguous fp32 [positions, d / 2, 2]")
     _need((gq is None) == (gk is None), "gq and gk: both or neither")
-    for g in (gq, gk):
-        _need(g is None or (g.dtype == torch.bfloat16 and g.is_contiguous() and g.numel() == d), "gq, gk: contiguous bf16 [d]")
-    _need(skipped is None or (skipped.dtype == torch.int32 and skipped.numel() == 1), "skipped: int32 [1]")
-    ld = qkv.stride(0) if rows > 1 else qkv.shape[1]
+    if gq is not None:
+        _need(all(g.dtype is torch.bfloat16 and g.is_contiguous() and g.shape == (d,) for g in (gq, gk)), "gq, gk: contiguous bf16 [d]")
+    _need(skipped is None or (skipped.dtype is torch.int32 and skipped.numel() == 1), "skipped: int32 [1]")
+    ld = qkv.stride(0) if rows > 1 else width
     _call(dev, "pat_op_kv_append", qkv.data_ptr(), _TYPE[qkv.dtype], ld, rows, hq, hkv, d, _list(seq, rows, "seq"), _list(pos, rows, "pos"),
-          cos_sin.data_ptr(), cos_sin.shape[0], gq.data_ptr() if gq is not None else None, gk.data_ptr() if gk is not None else None, eps,
+          cos_sin.data_ptr(), n_pos, gq.data_ptr() if gq is not None else None, gk.data_ptr() if gk is not None else None, eps,
           k_pages.data_ptr(), v_pages.data_ptr(), n_pages, P, page_table.data_ptr(), n_seqs, max_pages, q_out.data_ptr(), _rows(q_out, hq, d, "q_out"),
           skipped.data_ptr() if skipped is not None else None)
     return q_out
@@ -106,7 +112,7 @@ def pat_op_attn_plan(kv_len, group_start, shared_len, max_len, n_q_heads, n_kv_h
     their first shared_len[g] tokens (int32 [groups + 1] and [groups]).  plan: one to write anew (of as many sequences and the same heads), as a
     captured graph does."""
     n, ng = kv_len.shape[0], shared_len.shape[0]
-    dev = _on(kv_len, group_start, shared_len)
+    dev = _one_device(kv_len, group_start, shared_len)
     _need(1 <= n <= PAT_ATTN_MAX_SEQS and 1 <= ng <= PAT_ATTN_MAX_SEQS, f"1 .. {PAT_ATTN_MAX_SEQS} sequences and groups")
     if plan is None:
         lib = load_library()
@@ -122,7 +128,7 @@ def pat_op_attn_plan(kv_len, group_start, shared_len, max_len, n_q_heads, n_kv_h
 def pat_op_attn_shared(q, k_pages, v_pages, page_table, plan, out=None):
     """out [n, hq, d] = attention of one query token per sequence, q [n, hq, d], over the paged cache as the plan cuts it."""
     n_pages, hkv, P, d = _cache(k_pages, v_pages)
-    dev = _on(q, k_pages, v_pages, page_table, out, plan.buf)
+    dev = _one_device(q, k_pages, v_pages, page_table, out, plan.buf)
     n_seqs, max_pages = _table(page_table)
     n, hq = plan.n_seqs, plan.hq
     _need(plan.hkv == hkv and plan.d == d and n_seqs == n and q.shape[0] == n, "the plan is for other sequences or heads")
@@ -140,7 +146,7 @@ def pat_op_f8_pack_weight(w):
     """w [n, k] fp32 or bf16 -> (packed, scales): its 8-bit form, uint8 tensors as pat_op_f8_gemm reads them."""
     _need(w.dim() == 2 and w.dtype in _TYPE and w.stride(1) == 1, "w: fp32 or bf16 [n, k], rows dense")
     n, k = w.shape
-    dev, lib = _on(w), load_library()
+    dev, lib = _one_device(w), load_library()
     nbytes, sbytes = lib.pat_op_f8_weight_bytes(n, k), lib.pat_op_f8_scale_bytes(n, k)
     _need(nbytes > 0, f"n = {n}, k = {k}")
     packed, scales = (torch.empty(b, dtype=torch.uint8, device=dev) for b in (nbytes, sbytes))
@@ -152,15 +158,17 @@ def pat_op_f8_gemm(packed, scales, n, x, y=None, mode=0, y_dtype=None):
     """y [m, n] = (mode 0) or += (mode 1) x W^T for x [m, k] and the packed W [n, k]; y's type is x's unless y or y_dtype says otherwise."""
     _need(x.dim() == 2 and x.dtype in _TYPE and x.stride(1) == 1, "x: fp32 or bf16 [m, k], rows dense")
     m, k = x.shape
-    dev, lib = _on(x, packed, scales, y), load_library()
-    _need(packed.dtype == torch.uint8 and scales.dtype == torch.uint8 and packed.numel() == lib.pat_op_f8_weight_bytes(n, k) and scales.numel() == lib.pat_op_f8_scale_bytes(n, k),
-          f"packed weight and scales of a [{n}, {k}] matrix are needed")
+    dev, lib = _one_device(x, packed, scales, y), load_library()
+    if packed.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or packed.numel() != lib.pat_op_f8_weight_bytes(n, k) or scales.numel() != lib.pat_op_f8_scale_bytes(n, k) \
+            or not packed.is_contiguous() or not scales.is_contiguous():
+        _need(False, f"packed weight and scales of a [{n}, {k}] matrix are needed")
     if y is None:
         _need(mode == 0, "mode 1 adds to a given y")
         y = torch.empty(m, n, dtype=y_dtype or x.dtype, device=dev)
-    _need(y.dtype in _TYPE and tuple(y.shape) == (m, n) and y.stride(1) == 1, f"y: fp32 or bf16 [{m}, {n}], rows dense")
+    if y.dtype not in _TYPE or y.shape != (m, n) or y.stride(1) != 1:
+        _need(False, f"y: fp32 or bf16 [{m}, {n}], rows dense")
     nbytes = lib.pat_op_f8_gemm_scratch_bytes(n, k, m)
-    _need(nbytes >= 0, f"m = {m}")
+    _need(nbytes >= 0, "x: more rows than a call takes")
     scratch = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=dev)
     _call(dev, "pat_op_f8_gemm", packed.data_ptr(), scales.data_ptr(), n, k, x.data_ptr(), _TYPE[x.dtype], x.stride(0) if m > 1 else k, m, y.data_ptr(),
           _TYPE[y.dtype], y.stride(0) if m > 1 else n, mode, scratch.data_ptr())

@@ -1,0 +1,112 @@
+"""What the operators of include/pat_operators.h refuse, checked before anything reaches a GPU: no pointer here is ever followed."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2605_23945_amd as pat
+
+P = 0x10000                                                    # a well aligned address
+EINVAL, OK = pat.binding.PAT_EINVAL, pat.binding.PAT_OK
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return pat.load_library()
+
+
+APPEND = dict(qkv=P, type=0, ld=12 * 64, rows=0, hq=4, hkv=4, d=64, seq=P, pos=P, cs=P, n_pos=16, gq=None, gk=None, eps=1e-6, k=P, v=P, n_pages=8, page=16, table=P,
+              n_seqs=2, max_pages=2, q=P, ldq=4 * 64, skipped=None, stream=None)
+
+
+@pytest.mark.parametrize("bad", [dict(rows=-1), dict(type=2), dict(hq=0), dict(hkv=0), dict(hq=5000), dict(d=96), dict(page=48), dict(page=256), dict(n_pages=0), dict(ld=700), dict(ldq=255),
+                                 dict(ld=12 * 64 + 2), dict(ldq=4 * 64 + 1), dict(type=1, ld=12 * 64 + 4), dict(qkv=None), dict(seq=None), dict(pos=None), dict(cs=None),
+                                 dict(k=None), dict(v=None), dict(table=None), dict(q=None), dict(qkv=P + 4), dict(q=P + 8), dict(k=P + 2), dict(v=P + 8), dict(cs=P + 4), dict(n_pos=0),
+                                 dict(n_seqs=0), dict(max_pages=0), dict(gq=P), dict(gk=P), dict(eps=-1.0), dict(eps=float("nan")), dict(rows=1 << 30)])
+def test_append_refuses(lib, bad):
+    a = dict(APPEND, **{"rows": 1, **bad})
+    assert lib.pat_op_kv_append(*a.values()) == EINVAL
+
+
+def test_append_of_nothing_is_fine(lib):
+    assert lib.pat_op_kv_append(*APPEND.values()) == OK
+
+
+@pytest.mark.parametrize("bad", [(0, 64, 1e4, P), (16, 96, 1e4, P), (16, 64, 1.0, P), (16, 64, float("nan"), P), (16, 64, 1e4, None), (16, 64, 1e4, P + 4), (1 << 31, 64, 1e4, P)])
+def test_rope_table_refuses(lib, bad):
+    assert lib.pat_op_rope_table(*bad, None) == EINVAL
+
+
+PLAN = dict(kv_len=P, start=P, shared=P, n=4, groups=2, max_len=100, hq=8, hkv=2, plan=P, stream=None)
+ATTN = dict(q=P, type=1, ldq=8 * 64, n=4, hq=8, hkv=2, d=64, k=P, v=P, n_pages=4, page=16, table=P, max_pages=4, plan=P, out=P, ldo=8 * 64, scratch=P, stream=None)
+
+
+@pytest.mark.parametrize("bad", [dict(kv_len=None), dict(start=None), dict(shared=None), dict(plan=None), dict(plan=P + 4), dict(n=0), dict(n=2049), dict(groups=0), dict(groups=2049),
+                                 dict(max_len=0), dict(max_len=(1 << 30) + 1), dict(hq=7), dict(hkv=0), dict(hq=0), dict(hq=8192, hkv=8192)])
+def test_plan_refuses(lib, bad):
+    assert lib.pat_op_attn_plan(*dict(PLAN, **bad).values()) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(q=None), dict(k=None), dict(v=None), dict(table=None), dict(plan=None), dict(out=None), dict(scratch=None), dict(type=3), dict(d=32), dict(page=8),
+                                 dict(n_pages=0), dict(max_pages=0), dict(n=0), dict(n=2049), dict(hq=9), dict(ldq=511), dict(ldo=511), dict(ldq=8 * 64 + 4), dict(ldo=8 * 64 + 1),
+                                 dict(q=P + 2), dict(out=P + 8), dict(k=P + 8), dict(v=P + 4), dict(scratch=P + 128), dict(plan=P + 8)])
+def test_attention_refuses(lib, bad):
+    assert lib.pat_op_attn_shared(*dict(ATTN, **bad).values()) == EINVAL
+
+
+def test_attention_sizes(lib):
+    assert lib.pat_op_attn_plan_bytes(0, 8, 2) == -1 and lib.pat_op_attn_plan_bytes(4, 8, 3) == -1 and lib.pat_op_attn_plan_bytes(2049, 8, 2) == -1
+    assert lib.pat_op_attn_scratch_bytes(4, 8, 2, 96) == -1 and lib.pat_op_attn_scratch_bytes(4, 7, 2, 64) == -1
+    assert 0 < lib.pat_op_attn_plan_bytes(4, 8, 2) < lib.pat_op_attn_plan_bytes(4, 128, 2)       # more heads than a row block holds: more records
+    # a part per sequence and chunk: room for all sequences' shared and own ones beside the chunks
+    assert lib.pat_op_attn_scratch_bytes(2048, 8, 2, 64) >= 2 * 2048 * 8 * 66 * 4
+
+
+PACK = dict(w=P, type=1, ld=256, n=32, k=256, packed=P, scales=P, stream=None)
+GEMM = dict(w=P, ws=P, n=32, k=256, x=P, x_type=1, ldx=256, m=4, y=P, y_type=0, ldy=32, mode=0, scratch=P, stream=None)
+
+
+@pytest.mark.parametrize("bad", [dict(w=None), dict(packed=None), dict(scales=None), dict(type=2), dict(ld=255), dict(n=0), dict(k=0), dict(n=(1 << 22) + 1), dict(k=(1 << 20) + 1),
+                                 dict(packed=P + 16), dict(scales=P + 2), dict(w=P + 1), dict(type=0, w=P + 2)])
+def test_weight_packing_refuses(lib, bad):
+    assert lib.pat_op_f8_pack_weight(*dict(PACK, **bad).values()) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(w=None), dict(ws=None), dict(x=None), dict(y=None), dict(scratch=None), dict(x_type=2), dict(y_type=-1), dict(ldx=255), dict(ldy=31), dict(mode=2), dict(mode=-1),
+                                 dict(m=-1), dict(m=(1 << 19) + 1), dict(n=0), dict(k=0), dict(w=P + 128), dict(ws=P + 1), dict(x=P + 1), dict(y=P + 2), dict(scratch=P + 16)])
+def test_product_refuses(lib, bad):
+    assert lib.pat_op_f8_gemm(*dict(GEMM, **bad).values()) == EINVAL
+
+
+def test_product_of_nothing_is_fine(lib):
+    assert lib.pat_op_f8_gemm(*dict(GEMM, m=0, x=None, y=None, scratch=None).values()) == OK
+
+
+def test_product_sizes(lib):
+    assert lib.pat_op_f8_weight_bytes(1, 1) == 2048 and lib.pat_op_f8_weight_bytes(17, 129) == 4 * 2048 and lib.pat_op_f8_weight_bytes(0, 5) == -1
+    assert lib.pat_op_f8_scale_bytes(1, 1) == 4 and lib.pat_op_f8_scale_bytes(129, 513) == 16 and lib.pat_op_f8_scale_bytes(5, 0) == -1
+    assert lib.pat_op_f8_gemm_scratch_bytes(5, 5, -1) == -1 and lib.pat_op_f8_gemm_scratch_bytes(5, 5, 0) == 0
+    for n, k, m in ((4096, 11008, 251), (64, 28672, 100), (32000, 128, 70)):       # x's 8-bit form, its scales, the slices' sums
+        need = -(-m // 16) * 16 * (-(-k // 512) * 512 + -(-k // 512) * 4)
+        assert lib.pat_op_f8_gemm_scratch_bytes(n, k, m) >= need
+
+
+def test_the_binding_refuses_what_is_not_on_a_gpu_or_of_another_form():
+    f, i = torch.zeros, lambda *s: torch.zeros(*s, dtype=torch.int32)
+    k = f(2, 1, 16, 64, dtype=torch.bfloat16)
+    for call in (lambda: pat.pat_op_kv_append(f(1, 192), i(1), i(1), f(4, 32, 2), k, k.clone(), i(1, 2), f(1, 1, 64)),
+                 lambda: pat.pat_op_attn_plan(i(2), i(2), i(1), 10, 4, 4, 64),
+                 lambda: pat.pat_op_attn_shared(f(1, 1, 64), k, k.clone(), i(1, 2), pat.AttnPlan(f(4), 1, 1, 1, 64, 256)),
+                 lambda: pat.pat_op_f8_pack_weight(f(16, 16)),
+                 lambda: pat.pat_op_f8_gemm(f(8), f(8), 16, f(2, 16)),
+                 lambda: pat.pat_op_kv_append(f(1, 192), i(1), i(1), f(4, 32, 2), k.float(), k, i(1, 2), f(1, 1, 64)),
+                 lambda: pat.pat_op_f8_pack_weight(f(16, 16, dtype=torch.float16))):
+        with pytest.raises(pat.PatError) as e:
+            call()
+        assert e.value.code == EINVAL
+
+
+def test_types_of_the_binding_match_the_header(lib):
+    """Pointer-sized and 64-bit arguments are declared as such: a size beyond 2^31 comes back whole."""
+    assert lib.pat_op_f8_weight_bytes(1 << 20, 1 << 16) == 1 << 36
+    assert lib.pat_op_f8_gemm.argtypes[6] is C.c_int64 and lib.pat_op_kv_append.argtypes[2] is C.c_int64 and lib.pat_op_attn_shared.argtypes[15] is C.c_int64
