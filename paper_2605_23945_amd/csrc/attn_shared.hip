@@ -71,6 +71,9 @@ __device__ __forceinline__ int find(const int32_t *off, int n, int x)
     return lo;
 }
 
+// how many records on, at n workgroups each dealt to eight XCDs in turn, a workgroup of the same XCD comes
+__device__ __forceinline__ int xcd_stride(int n) { return (n & 7) == 0 ? 1 : 8 / (n & -n); }
+
 __device__ __forceinline__ int up(int64_t v, int to) { return (int)((v + to - 1) / to * to); }
 
 // One workgroup.  A group shares its prefix if at least two of its sequences reach its end; others, and sequences shorter
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(kPlan) void attn_plan_kernel(SharedPlanArgs a)
     }
     // A chunk's row blocks read the same keys: they come D records apart, so that their workgroups, hkv to a record and dealt to the eight XCDs in
     // turn, share an XCD's L2.
-    const int D = 8 / ((a.hkv & 7) == 0 ? 8 : a.hkv & -a.hkv);
+    const int D = xcd_stride(a.hkv);
     for (int r = tid; r < np; r += kPlan) {
         const int g = find(grec, ng, r), k = r - grec[g], lo = a.group_start[g], members = a.group_start[g + 1] - lo;
         const int nb = (members * G + kSharedRows - 1) / kSharedRows, nc = (a.shared_len[g] + CP - 1) / CP;
@@ -487,12 +490,18 @@ __global__ __launch_bounds__(kW * 64, 2) void attn_shared_kernel(SharedArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // fp32 queries, three terms each, leave registers for one row tile of 16: a record's second tile is an item of its own
     const int halves = F32 ? 2 : 1, own_halves = F32 && a.hq / hkv > 16 ? 2 : 1;
+    const int D8 = xcd_stride(hkv);
     const int64_t first_own = (int64_t)np * hkv * halves, items = first_own + (int64_t)no * per * own_halves;
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
         const bool prefix = it < first_own;
-        uint32_t x = (uint32_t)(prefix ? it : it - first_own);
-        const uint32_t div = prefix ? hkv : per, of = (prefix ? np : no) * div, half = F32 && x >= of ? 1 : 0;
-        x -= half * of;
+        uint32_t x = (uint32_t)(prefix ? it : it - first_own), half = 0;
+        const uint32_t div = prefix ? hkv : per, of = prefix ? np : no;
+        if (F32 && (prefix || own_halves > 1)) {               // D records' first tiles, then their second ones, which read the same keys on the same XCD
+            const uint32_t blk = x / (2 * D8 * div), w = min((uint32_t)D8, of - blk * D8) * div;
+            x -= blk * 2 * D8 * div;
+            half = x >= w ? 1 : 0;
+            x += blk * D8 * div - half * w;
+        }
         const uint32_t ri = x / div;
         const bool together = prefix || !solo;
         const int h = (int)(x - ri * div) * (together ? 1 : kW) + (together ? 0 : wave);

@@ -9,6 +9,8 @@ from .binding import PAT_EINVAL, PatError, load_library
 
 _TYPE = {torch.float32: 0, torch.bfloat16: 1}
 PAT_ATTN_MAX_SEQS = 2048
+# a device's current stream as a number: torch's own short cut where it has it, a microsecond of ten less on a small call
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _need(ok, what):
@@ -31,9 +33,9 @@ def _call(dev, name, *args):
     fn, at = getattr(load_library(), name), dev.index
     if torch.cuda.current_device() != at:
         with torch.cuda.device(at):
-            rc = fn(*args, torch.cuda.current_stream(at).cuda_stream)
+            rc = fn(*args, _stream(at))
     else:
-        rc = fn(*args, torch.cuda.current_stream(at).cuda_stream)
+        rc = fn(*args, _stream(at))
     if rc:
         raise PatError(rc, name)
 
