@@ -325,7 +325,15 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
 #pragma unroll
         for (int f = 0; f < FT; ++f) o[t][f] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     }
-    const char *kt = ring, *vt = ring + kHalf;
+    // the lane's places in K's and V's tiles; a key 16 further on has the same permutation
+    const char *kat[KST], *vat[FT];
+    {
+        const int ka = g4 * 4 + (col >> 2);                    // key whose pieces this lane addresses
+#pragma unroll
+        for (int ks = 0; ks < KST; ++ks) kat[ks] = ring + (col * PC + ((ks * 4 + g4) ^ (col & (PC - 1)))) * 16;
+#pragma unroll
+        for (int f = 0; f < FT; ++f) vat[f] = ring + kHalf + (ka * PC + ((f * 2 + ((col & 3) >> 1)) ^ (ka & (PC - 1)))) * 16 + (col & 1) * 8;
+    }
     for (int i = 0; i < n; ++i) {
         const int key0 = tb + (i * ws + w0) * kTile;
         wait_newer<NI>();                                      // newer than this tile's K: its V
@@ -333,10 +341,7 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int ks = 0; ks < KST; ++ks) {
-                const int key = j * 16 + col;
-                kf[j][ks] = *reinterpret_cast<const u32x4_t *>(kt + (key * PC + ((ks * 4 + g4) ^ (key & (PC - 1)))) * 16);
-            }
+            for (int ks = 0; ks < KST; ++ks) kf[j][ks] = *reinterpret_cast<const u32x4_t *>(kat[ks] + j * 16 * PC * 16);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // read: the place can be requested anew
         if (i + 1 < n) {
             if (((i + 1) & 31) == 0) look_up(i + 1);
@@ -373,7 +378,9 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
             for (int j = 1; j < 8; ++j) mt = fmaxf(mt, p[j]);
             mt = column_max(mt);
             const float Mn = fmaxf(M[t], mt * scale);
-            if (__any(Mn > M[t])) {                            // some row of the tile has a new maximum
+            // Weights are formed in the unit of a maximum seen, not always the last one: up to 2^8 they lose nothing in fp32, and sums are
+            // brought to a new unit only where some row's scores pass it by more
+            if (__any(Mn > M[t] + 8.f)) {
                 const float corr = M[t] == Mn ? 1.f : __builtin_amdgcn_exp2f(M[t] - Mn);     // exp2(-inf) = 0 on the wave's first keys
                 M[t] = Mn;
                 den[t] *= corr;
@@ -387,13 +394,10 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
             else split2_bf16(p, ph[t], pm[t]);
         }
         if (i + 1 < n) wait_newer<NI>(); else wait_newer<0>(); // newer than this tile's V: the K requested above
-        const int ka = g4 * 4 + (col >> 2), kb = ka + 16;      // keys whose pieces this lane addresses
         u32x4_t vf[FT];
 #pragma unroll
         for (int f = 0; f < FT; ++f) {
-            const int piece = f * 2 + ((col & 3) >> 1), half = (col & 1) * 8;
-            const uint2 va = lds_read_tr(vt + (ka * PC + (piece ^ (ka & (PC - 1)))) * 16 + half);
-            const uint2 vb = lds_read_tr(vt + (kb * PC + (piece ^ (kb & (PC - 1)))) * 16 + half);
+            const uint2 va = lds_read_tr(vat[f]), vb = lds_read_tr(vat[f] + 16 * PC * 16);
             vf[f] = u32x4_t{va.x, va.y, vb.x, vb.y};
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -605,7 +609,7 @@ hipError_t launch_shared(const SharedArgs &a, int n_cu, hipStream_t s)
     typedef typename std::conditional<F32, float, uint16_t>::type E;
     const int G = a.hq / a.hkv;
     const int64_t items = shared_records(a.n_seqs, G) * a.hkv;
-    const unsigned grid = (unsigned)(items < 8 * n_cu ? items : 8 * n_cu);
+    const unsigned grid = (unsigned)(items < 16 * n_cu ? items : 16 * n_cu);
     attn_shared_kernel<D, F32><<<grid, kW * 64, kW * kTile * D * 4, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
