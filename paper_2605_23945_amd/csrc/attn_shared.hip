@@ -492,21 +492,10 @@ __global__ __launch_bounds__(kW * 64, 2) void attn_shared_kernel(SharedArgs a)
     if (!made_for(head, a)) return;
     const int np = head->n_prefix, no = head->n_own, solo = head->solo, hkv = a.hkv, per = solo ? hkv / kW : hkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // fp32 queries, three terms each, leave registers for one row tile of 16: a record's second tile is an item of its own
-    const int halves = F32 ? 2 : 1, own_halves = F32 && a.hq / hkv > 16 ? 2 : 1;
-    const int D8 = xcd_stride(hkv);
-    const int64_t first_own = (int64_t)np * hkv * halves, items = first_own + (int64_t)no * per * own_halves;
+    const int64_t first_own = (int64_t)np * hkv, items = first_own + (int64_t)no * per;
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
         const bool prefix = it < first_own;
-        uint32_t x = (uint32_t)(prefix ? it : it - first_own), half = 0;
-        const uint32_t div = prefix ? hkv : per, of = prefix ? np : no;
-        if (F32 && (prefix || own_halves > 1)) {               // D records' first tiles, then their second ones, which read the same keys on the same XCD
-            const uint32_t blk = x / (2 * D8 * div), w = min((uint32_t)D8, of - blk * D8) * div;
-            x -= blk * 2 * D8 * div;
-            half = x >= w ? 1 : 0;
-            x += blk * D8 * div - half * w;
-        }
-        const uint32_t ri = x / div;
+        const uint32_t x = (uint32_t)(prefix ? it : it - first_own), div = prefix ? hkv : per, ri = x / div;
         const bool together = prefix || !solo;
         const int h = (int)(x - ri * div) * (together ? 1 : kW) + (together ? 0 : wave);
         const SharedRecord *rp = recs + (prefix ? ri : np + ri);
@@ -514,12 +503,14 @@ __global__ __launch_bounds__(kW * 64, 2) void attn_shared_kernel(SharedArgs a)
         e.seq0 = __builtin_amdgcn_readfirstlane(rp->seq0); e.r0 = __builtin_amdgcn_readfirstlane(rp->r0); e.rows = __builtin_amdgcn_readfirstlane(rp->rows);
         e.table_row = __builtin_amdgcn_readfirstlane(rp->table_row); e.t0 = __builtin_amdgcn_readfirstlane(rp->t0); e.cnt = __builtin_amdgcn_readfirstlane(rp->cnt);
         e.part0 = __builtin_amdgcn_readfirstlane(rp->part0);
-        if (F32) {
-            e.r0 += half * 16;
-            e.rows = min(16, e.rows - (int)half * 16);
-            if (e.rows <= 0) continue;
+        if constexpr (F32) {
+            // fp32 queries, three terms each, leave registers for one row tile of 16: the second reads the keys again, from L2
+            const int rows = e.rows;
+            for (int r = 0; r < rows; r += 16, e.r0 += 16) {
+                e.rows = min(16, rows - r);
+                item<D, 1, true>(a, e, h, together, !prefix && rows <= 16, lds, wml);
+            }
         }
-        if constexpr (F32) item<D, 1, F32>(a, e, h, together, !prefix, lds, wml);
         else if (e.rows <= 16) item<D, 1, F32>(a, e, h, together, !prefix, lds, wml);
         else item<D, 2, F32>(a, e, h, together, !prefix, lds, wml);
     }
