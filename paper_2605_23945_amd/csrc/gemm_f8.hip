@@ -249,9 +249,9 @@ __device__ __forceinline__ void emit(const F8Args &a, int m, int n0, floatx4_t v
 // ---- few rows: weights streamed once, straight into registers ------------------------------------------------------
 // A workgroup holds TN tiles of 16 weight rows; its eight waves take the blocks of columns in turn (wave w: w, w + 8, ...) and their
 // sums meet in LDS, added in wave order.  A wave keeps three blocks' operands in registers (two above 32 rows), all but one of them on their way: a block's weights and its part of x
-// are requested together, since loads arrive in order.  Up to 16 rows (RAW) every wave brings x to its 8-bit form
+// are requested together, since loads arrive in order.  Where x is small (RAW) every wave brings it to its 8-bit form
 // itself, in the registers the product reads it from: lanes r, r + 16, r + 32 and r + 48 hold row r's block; no launch, no scratch and no barrier
-// precede the stream.  Above, x comes packed.
+// precede the stream.  Elsewhere x comes packed.
 constexpr int kStreamWaves = 8;
 
 __device__ __forceinline__ v8i_t both(u32x4_t a, u32x4_t b) { return v8i_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]}; }
@@ -527,6 +527,7 @@ hipError_t launch_product(const F8Args &a, hipStream_t s)
     const int MT = a.Mp / 16;
     if (MT <= 4) {
         switch (MT) {
+        case 1: return launch_stream<1, false, float, E>(a, nullptr, 0, 0, false, s);
         case 2: return launch_stream<2, false, float, E>(a, nullptr, 0, 0, false, s);
         case 3: return launch_stream<3, false, float, E>(a, nullptr, 0, 0, false, s);
         default: return launch_stream<4, false, float, E>(a, nullptr, 0, 0, false, s);
@@ -553,7 +554,7 @@ F8Tile f8_tile(int n, int m, int KB, bool wide)
         for (int sl = 1; sl <= 8 && sl <= KB4; ++sl) {         // a slice has a word of scales at least
             const int64_t wg = (int64_t)((NT + tn - 1) / tn) * mblk * sl;
             const double block = wide ? 0.7 : 0.17 + 0.048 * tn;
-            const double cost = (double)((wg + 255) / 256) * ((KB4 + sl - 1) / sl * 4) * block + (sl > 1 ? 2.5 + (double)m * n * sl * 8 / 6e6 : 0.0);
+            const double cost = (double)((wg + 255) / 256) * ((KB4 + sl - 1) / sl * 4) * block + (sl > 1 ? 4.5 + (double)m * n * sl * 8 / 6e6 : 0.0);
             if (cost < least) { least = cost; best = F8Tile{tn, sl}; }
         }
     return best;

@@ -136,7 +136,9 @@ int pat_op_f8_gemm(const void *w_packed, const void *w_scales, int32_t n, int32_
     a.y = y; a.ldy = ldy; a.n = n; a.m = m; a.Mp = (m + 15) / 16 * 16; a.KB = (k + 127) / 128; a.add = mode == 1;
     a.part = (float *)((char *)scratch + part_offset(m, k));
     a.vec = aligned(y, 4 * size_of(y_type)) && ldy % 4 == 0;
-    if (m <= 16) return done(launch_f8_gemm_raw(a, x, x_type == PAT_F32, ldx, k, y_type == PAT_F32, (hipStream_t)stream));
+    // Every workgroup reads x whole.  Up to 64 KiB of it the product's waves bring it to 8 bits themselves (one row of 4096 x 12288: 11.4 us, 12.8 with a launch
+    // before it); above, what that costs each workgroup passes the launch (16 rows of 4096 x 22016: 22.2 and 19.8 us).
+    if (m <= 16 && (int64_t)m * k * size_of(x_type) <= 65536) return done(launch_f8_gemm_raw(a, x, x_type == PAT_F32, ldx, k, y_type == PAT_F32, (hipStream_t)stream));
     const hipError_t e = launch_f8_pack_act(x, x_type == PAT_F32, ldx, m, k, scratch, sc, (hipStream_t)stream);
     return e != hipSuccess ? PAT_EHIP : done(launch_f8_gemm(a, y_type == PAT_F32, (hipStream_t)stream));
 }

@@ -96,7 +96,7 @@ inline int64_t f8_part_bytes(int n, int m, int k)
 hipError_t launch_f8_pack_act(const void *x, bool f32, int64_t ld, int m, int k, void *packed, void *scales, hipStream_t s);
 hipError_t launch_f8_pack_weight(const void *w, bool f32, int64_t ld, int n, int k, void *packed, void *scales, hipStream_t s);
 hipError_t launch_f8_gemm(const F8Args &a, bool f32, hipStream_t s);
-// up to 16 rows: x as it is, brought to its 8-bit form by the product's own waves (F8Args::x, xs unused)
+// up to 16 rows, x as it is, brought to its 8-bit form by the product's own waves (F8Args::x, xs unused)
 hipError_t launch_f8_gemm_raw(const F8Args &a, const void *x, bool x32, int64_t ldx, int k, bool y32, hipStream_t s);
 
 }  // namespace pat

@@ -50,7 +50,7 @@ def test_types(pat, m, x_dtype, y_dtype):
     _check(pat, m, 384, 512, x_dtype, y_dtype)
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 4096, 4096), (8, 12288, 1024), (27, 5120, 2048), (64, 2048, 6912), (251, 4096, 4096), (600, 3000, 1111), (1500, 7168, 1024),
+@pytest.mark.parametrize("m,n,k", [(1, 4096, 4096), (8, 12288, 1024), (16, 8208, 2048), (16, 8208, 2176), (5, 3000, 28672), (12, 300, 6912), (40, 24000, 300), (27, 5120, 2048), (64, 2048, 6912), (251, 4096, 4096), (600, 3000, 1111), (1500, 7168, 1024),
                                    (5003, 1024, 1024), (40, 32000, 256), (16, 256, 28672), (300, 200, 11008)])
 def test_larger_products(pat, m, n, k):
     _check(pat, m, n, k, torch.bfloat16, torch.float32, rows=sorted({0, m // 3, m // 2, m - 1}), seed=5)
