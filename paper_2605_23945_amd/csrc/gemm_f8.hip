@@ -188,7 +188,9 @@ __global__ __launch_bounds__(256) void f8_pack_weight_kernel(const E *w, int64_t
         const int row = nb * 128 + i * 32 + (threadIdx.x >> 3), tile = row >> 4;
         if (tile < (n + 15) / 16) packed[((int64_t)tile * KB + kb) * 128 + (piece >> 2) * 64 + (piece & 3) * 16 + (row & 15)] = to_f8(v[i], code, fin);
     }
-    if (threadIdx.x == 0) scales[((int64_t)nb * KB4 + (kb >> 2)) * 4 + (kb & 3)] = (uint8_t)code;
+    // the rest of a row's last word is 2^0: the products' padding multiplies by it, and a byte left as it was could be the scale that is no number
+    if (threadIdx.x == 0)
+        for (int i = kb; i < (kb == KB - 1 ? KB4 * 4 : kb + 1); ++i) scales[(int64_t)nb * KB4 * 4 + i] = (uint8_t)(i == kb ? code : 127);
 }
 
 __device__ __forceinline__ v8i_t both(uint4 a, uint4 b) { return v8i_t{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w}; }
@@ -347,18 +349,18 @@ __global__ __launch_bounds__(kStreamWaves * 64) void f8_stream_kernel(F8Args a, 
 }
 
 // ---- many rows: tiles on the matrix cores ------------------------------------------------------------------------------
-// A workgroup holds TN tiles of 16 weight rows and 8 tiles of 16 batch rows, a wave all TN and two of the batch's: weights go through LDS
-// (asynchronous loads, S stages of TN x 2 KiB), where the four waves share them; the batch's tiles are one wave's alone and go straight to
+// A workgroup of W waves holds TN tiles of 16 weight rows and 2 W tiles of 16 batch rows, a wave all TN and two of the batch's: weights go through LDS
+// (asynchronous loads, S stages of TN x 2 KiB), where the waves share them; the batch's tiles are one wave's alone and go straight to
 // registers, three blocks of columns ahead (x has just been written, so it comes from beyond the XCD's own L2).  Towards the end
 // of a block all waves meet: the next block's weights have arrived, and the stage just read is requested anew.  Loads arrive in order,
 // so a wave waits for its weights by the number of loads that it has issued since.
 // The loop takes four blocks a turn, which one word of scales covers; K is padded to that with blocks of x that are zero.  There is no branch
 // in it: the compiler moves matrix products past one.
-constexpr int kBatchTiles = 2;      // four, and workgroups of 256 rows: 287 us where two take 286 (5003 x 7168 x 8192), more at every smaller batch
-template <int TN, int S, typename E>
-__global__ __launch_bounds__(256, 2) void f8_tile_kernel(F8Args a, int nblk, int mblk, int slices)
+constexpr int kBatchTiles = 2;      // four: 287 us where two take 286 (5003 x 7168 x 8192), more at every smaller batch
+template <int TN, int W, int S, typename E>
+__global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, int mblk, int slices)
 {
-    constexpr int TM = kBatchTiles, kStage = TN * 2048, NJ = TN / 2;      // load instructions of a wave per stage
+    constexpr int TM = kBatchTiles, kStage = TN * 2048, NJ = 2 * TN / W;      // load instructions of a wave per stage
     constexpr int kAhead = 3;                                  // weight tiles in registers on their way from LDS: one tile's products are shorter than its read
     constexpr bool WIDE = sizeof(E) == 4;
     __shared__ __align__(16) char lds[S * kStage];
@@ -391,7 +393,7 @@ __global__ __launch_bounds__(256, 2) void f8_tile_kernel(F8Args a, int nblk, int
     const uint32_t *xss[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int mt = min((mb * 4 + wave) * TM + i, MT - 1);
+        const int mt = min((mb * W + wave) * TM + i, MT - 1);
         xsrc[i] = reinterpret_cast<const u32x4_t *>(a.x) + (int64_t)mt * KB4 * 512 + lane;
         xss[i] = a.xs + mt * 16 + col;
     }
@@ -470,7 +472,7 @@ __global__ __launch_bounds__(256, 2) void f8_tile_kernel(F8Args a, int nblk, int
         for (int t = 0; t < TN; ++t)
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                const int mt = (mb * 4 + wave) * TM + i, nt = nb * TN + t;
+                const int mt = (mb * W + wave) * TM + i, nt = nb * TN + t;
                 if (mt < MT && nt < NT) *reinterpret_cast<floatx4_t *>(part + ((int64_t)(mt * 16 + col) * NT + nt) * 16 + g * 4) = acc[t][i];
             }
         return;
@@ -480,7 +482,7 @@ __global__ __launch_bounds__(256, 2) void f8_tile_kernel(F8Args a, int nblk, int
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             __builtin_amdgcn_sched_barrier(0);
-            emit<E>(a, ((mb * 4 + wave) * TM + i) * 16 + col, (nb * TN + t) * 16 + g * 4, acc[t][i]);
+            emit<E>(a, ((mb * W + wave) * TM + i) * 16 + col, (nb * TN + t) * 16 + g * 4, acc[t][i]);
         }
 }
 
@@ -501,11 +503,11 @@ __global__ __launch_bounds__(256) void f8_join_kernel(F8Args a, int slices)
     emit<E>(a, m, n4 * 4, v);
 }
 
-template <int TN, int S, typename E>
+template <int TN, int W, int S, typename E>
 hipError_t launch_tile(const F8Args &a, int slices, hipStream_t s)
 {
-    const int NT = (a.n + 15) / 16, nblk = (NT + TN - 1) / TN, mblk = (a.m + 127) / 128;
-    f8_tile_kernel<TN, S, E><<<(unsigned)(nblk * mblk * slices), 256, 0, s>>>(a, nblk, mblk, slices);
+    const int NT = (a.n + 15) / 16, nblk = (NT + TN - 1) / TN, mblk = (a.m + W * 32 - 1) / (W * 32);
+    f8_tile_kernel<TN, W, S, E><<<(unsigned)(nblk * mblk * slices), W * 64, 0, s>>>(a, nblk, mblk, slices);
     if (slices > 1) f8_join_kernel<E><<<(unsigned)(((int64_t)a.m * NT * 4 + 255) / 256), 256, 0, s>>>(a, slices);
     return hipGetLastError();
 }
@@ -534,29 +536,31 @@ hipError_t launch_product(const F8Args &a, hipStream_t s)
         }
     }
     const F8Tile t = f8_tile(a.n, a.m, a.KB, sizeof(E) == 4);
-    if constexpr (sizeof(E) == 4) return launch_tile<4, 4, E>(a, t.slices, s);
-    else return t.TN == 12 ? launch_tile<12, 3, E>(a, t.slices, s) : t.TN == 8 ? launch_tile<8, 4, E>(a, t.slices, s) : launch_tile<4, 4, E>(a, t.slices, s);
+    if constexpr (sizeof(E) == 4) return launch_tile<4, 4, 4, E>(a, t.slices, s);
+    else if (t.W == 8) return t.TN == 12 ? launch_tile<12, 8, 4, E>(a, t.slices, s) : launch_tile<8, 8, 4, E>(a, t.slices, s);
+    else return t.TN == 12 ? launch_tile<12, 4, 3, E>(a, t.slices, s) : t.TN == 8 ? launch_tile<8, 4, 4, E>(a, t.slices, s) : launch_tile<4, 4, 4, E>(a, t.slices, s);
 }
 
 }  // namespace
 
-// Weight tiles of a workgroup and cuts of K.  A workgroup keeps a compute unit's matrix pipes about as busy as two do, so the time is rounds of
-// 256 workgroups, blocks of columns in each and 0.17 + 0.048 TN us a block (0.36, 0.55 and 0.75 us for 4, 8 and 12, by products of 128 to 5003
-// rows), 0.7 us for fp32 results; a cut K costs a launch and its sums' way out and back.  Between 251 x 22016 x 4096 (12 tiles 34 us, 8 42, 4 41),
-// 128 x 22016 x 4096 (31, 27, 31), 100 x 12288 x 4096 (27, 20, 16) and 251 x 4096 x 11008 (two slices of 4 tiles 26 us, four of 8 27, one 37) the rule
-// takes the best of each.
+// Weight tiles and waves of a workgroup and cuts of K.  A workgroup keeps a compute unit about as busy as two do, so the time is rounds of
+// 256 workgroups, blocks of columns in each and a block's time: 0.36, 0.55 and 0.75 us for 4, 8 and 12 tiles by four waves, 1.0 and 1.37 us for 8 and 12 by eight
+// (measured on products of 100 to 5003 rows), 0.7 us for fp32 results; a cut K costs a launch and its sums' way out and back.  Measured, 5003 x 7168 x 8192: 12 tiles by
+// eight waves 269 us, by four 286, 8 tiles 287 and 295; 2048 x 8192 x 8192: 155, 139, 125 and 136; 128 x 22016 x 4096: 40, 31, 32 and 27, 4 tiles 31;
+// 100 x 12288 x 4096: 35, 26, 25 and 20, 4 tiles 16; 251 x 4096 x 11008: two slices of 4 tiles 26, four of 8 27, one of 4 37.  The rule takes the best of each.
 F8Tile f8_tile(int n, int m, int KB, bool wide)
 {
-    const int NT = (n + 15) / 16, mblk = (m + 127) / 128, KB4 = (KB + 3) / 4;
-    F8Tile best{4, 1};
+    const int NT = (n + 15) / 16, KB4 = (KB + 3) / 4;
+    F8Tile best{4, 4, 1};
     double least = 1e300;
-    for (int tn = 4; tn <= (wide ? 4 : 12); tn += 4)
-        for (int sl = 1; sl <= 8 && sl <= KB4; ++sl) {         // a slice has a word of scales at least
-            const int64_t wg = (int64_t)((NT + tn - 1) / tn) * mblk * sl;
-            const double block = wide ? 0.7 : 0.17 + 0.048 * tn;
-            const double cost = (double)((wg + 255) / 256) * ((KB4 + sl - 1) / sl * 4) * block + (sl > 1 ? 4.5 + (double)m * n * sl * 8 / 6e6 : 0.0);
-            if (cost < least) { least = cost; best = F8Tile{tn, sl}; }
-        }
+    for (int w = 4; w <= (wide ? 4 : 8); w += 4)
+        for (int tn = w; tn <= (wide ? 4 : 12); tn += 4)
+            for (int sl = 1; sl <= 8 && sl <= KB4; ++sl) {     // a slice has a word of scales at least
+                const int64_t wg = (int64_t)((NT + tn - 1) / tn) * ((m + 32 * w - 1) / (32 * w)) * sl;
+                const double block = wide ? 0.7 : w == 4 ? 0.17 + 0.048 * tn : 0.22 + 0.096 * tn;
+                const double cost = (double)((wg + 255) / 256) * ((KB4 + sl - 1) / sl * 4) * block + (sl > 1 ? 5.0 + (double)m * n * sl * 8 / 4e6 : 0.0);
+                if (cost < least) { least = cost; best = F8Tile{tn, w, sl}; }
+            }
     return best;
 }
 

@@ -85,7 +85,7 @@ struct F8Args {
     bool add, vec;             // y += ; rows n .. n + 3 of y by one store
     float *part;               // sums of K slices [slice][Mp][16-row tiles of n][16], where f8_tile has more than one
 };
-struct F8Tile { int TN, slices; };         // above 64 rows: tiles of weight rows per workgroup, cuts of K
+struct F8Tile { int TN, W, slices; };      // above 64 rows: tiles of weight rows per workgroup, waves of 32 batch rows, cuts of K
 F8Tile f8_tile(int n, int m, int KB, bool wide);      // wide: fp32 results
 inline int64_t f8_part_bytes(int n, int m, int k)
 {

@@ -50,10 +50,13 @@ def test_types(pat, m, x_dtype, y_dtype):
     _check(pat, m, 384, 512, x_dtype, y_dtype)
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 4096, 4096), (8, 12288, 1024), (16, 8208, 2048), (16, 8208, 2176), (5, 3000, 28672), (12, 300, 6912), (40, 24000, 300), (27, 5120, 2048), (64, 2048, 6912), (251, 4096, 4096), (600, 3000, 1111), (1500, 7168, 1024),
-                                   (5003, 1024, 1024), (40, 32000, 256), (16, 256, 28672), (300, 200, 11008)])
-def test_larger_products(pat, m, n, k):
-    _check(pat, m, n, k, torch.bfloat16, torch.float32, rows=sorted({0, m // 3, m // 2, m - 1}), seed=5)
+@pytest.mark.parametrize("y_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,n,k", [(1, 4096, 4096), (8, 12288, 1024), (16, 8208, 2048), (16, 8208, 2176), (5, 3000, 28672), (12, 300, 6912), (40, 24000, 300), (27, 5120, 2048), (64, 2048, 6912),
+                                   (251, 4096, 4096), (600, 3000, 1111), (1500, 7168, 1024), (5003, 1024, 1024), (40, 32000, 256), (16, 256, 28672), (300, 200, 11008),
+                                   (120, 20000, 300), (1000, 7170, 700), (700, 12304, 520), (300, 11008, 256), (100, 300, 5000), (70, 100, 6912)])
+def test_larger_products(pat, m, n, k, y_dtype):
+    """Every tile of weights, one to eight of them a workgroup, four and eight waves, K whole and in slices, ends inside tiles."""
+    _check(pat, m, n, k, torch.bfloat16, y_dtype, rows=sorted({0, m // 3, m // 2, m - 1}), seed=5)
 
 
 def test_the_forms_are_bit_exact(pat):
@@ -121,6 +124,19 @@ def test_adding_to_y_and_rows_with_strides(pat, m, n, k, dtype):
 def test_no_rows(pat):
     pw = pat.pat_op_f8_pack_weight(_x((32, 64), 1).to(DEV))
     assert pat.pat_op_f8_gemm(*pw, 32, torch.empty(0, 64, device=DEV)).shape == (0, 32)
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 300, 130), (40, 300, 520), (300, 300, 640), (700, 12304, 520)])
+def test_scales_of_the_padding_are_set(pat, m, n, k):
+    """A weight's scales go four to a word: what a shorter last word holds beside them is defined, whatever was in the memory before."""
+    lib = pat.load_library()
+    w, x = _x((n, k), 1, torch.bfloat16, 0.05).to(DEV), _x((m, k), 2, torch.bfloat16).to(DEV)
+    packed, scales = pat.pat_op_f8_pack_weight(w)
+    again = torch.full_like(scales, 255)
+    assert lib.pat_op_f8_pack_weight(w.data_ptr(), 1, k, n, k, packed.data_ptr(), again.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(scales, again)
+    for y_dtype in (torch.float32, torch.bfloat16):
+        assert bool(torch.isfinite(pat.pat_op_f8_gemm(packed, again, n, x, y_dtype=y_dtype)).all())
 
 
 @pytest.mark.parametrize("m", [1, 40, 300])
