@@ -32,7 +32,7 @@ extern "C" {
 #define PAT_BF16 1
 
 /* cos_sin[pos][j] = (cos, sin) of pos * base^(-2 j / head_dim), j < head_dim / 2, formed in 64 bits: float[n_pos][head_dim / 2][2],
- * 16-byte aligned.  A program makes it once. */
+ * 16-byte aligned, n_pos <= 2^25.  A program makes it once. */
 int pat_op_rope_table(int64_t n_pos, int32_t head_dim, double base, float *cos_sin, void *hip_stream);
 
 /* Row i of qkv [rows, ld] (ld elements from row to row) holds the n_q_heads q heads, then the n_kv_heads k heads, then the
@@ -40,7 +40,7 @@ int pat_op_rope_table(int64_t n_pos, int32_t head_dim, double base, float *cos_s
  * prefilled, in any order.  With gains gq, gk (bf16 [head_dim], both or neither) each q and k head first gets an RMSNorm
  * with epsilon eps.  q and k heads are rotated: features (j, j + head_dim / 2) by the angle of (pos[i], j).  q goes to row i of
  * q_out [rows, ldq] in qkv's type (it may be qkv itself with ldq = ld), k and v rounded to the cache.
- *   16-byte alignment: qkv, q_out, cos_sin, the pools, and ld and ldq in bytes.
+ *   16-byte alignment: qkv, q_out, cos_sin, the pools, and ld and ldq in bytes.  rows * (heads of a row) < 2^28.
  *   seq[i] < 0 is a row of padding: nothing is read or written for it.
  *   seq[i] >= n_seqs, pos[i] outside [0, n_pos) or the table's row, a page id outside [0, n_pages): nothing is written for the row,
  *   and *skipped (device, or NULL) is raised by one.
@@ -63,8 +63,8 @@ int pat_op_kv_append(const void *qkv, int32_t type, int64_t ld, int32_t rows, in
  * group_start that is no such list, gives NaN as the result of the sequence, or of all, and so does a page id outside
  * [0, n_pages) or a length beyond max_pages, of the sequences that need the page.
  *
- * pat_op_attn_shared: q [n_seqs, ldq] and out [n_seqs, ldo], n_q_heads * head_dim used, of one type; scores q k / sqrt(head_dim);
- * 16-byte alignment (q, out, pools, ldq and ldo in bytes); scratch pat_op_attn_scratch_bytes() bytes, 256-byte aligned,
+ * pat_op_attn_shared: q [n_seqs, ldq] and out [n_seqs, ldo], n_q_heads * head_dim used, of one type (out may be q itself with ldo = ldq); scores
+ * q k / sqrt(head_dim); 16-byte alignment (q, out, pools, ldq and ldo in bytes); scratch pat_op_attn_scratch_bytes() bytes, 256-byte aligned,
  * overwritten, so calls that overlap in time need one each.  A plan is only read.  A sequence's result does not depend on
  * the values of keys behind its end.  A plan made for another n_seqs, n_q_heads or n_kv_heads gives NaN throughout. */
 int64_t pat_op_attn_plan_bytes(int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads);
@@ -82,9 +82,11 @@ int pat_op_attn_shared(const void *q, int32_t type, int64_t ldq, int32_t n_seqs,
  *
  * pat_op_f8_pack_weight brings w [n, k] (ld elements from row to row) into that form, once: packed (256-byte aligned)
  * pat_op_f8_weight_bytes() bytes, scales (4-byte aligned) pat_op_f8_scale_bytes() bytes.
- * pat_op_f8_gemm: y [m, ldy] = (mode 0) or += (mode 1) x W^T for x [m, ldx], both of any type code, any n, k, m >= 1 (m = 0 does
- * nothing): x is brought to its 8-bit form on the way, products and sums are fp32, the result is rounded once.
- * scratch: pat_op_f8_gemm_scratch_bytes() bytes, 256-byte aligned, overwritten.  y must not overlap x. */
+ * pat_op_f8_gemm: y [m, ldy] = (mode 0) or += (mode 1) x W^T for x [m, ldx], both of any type code (m = 0 does nothing): x is
+ * brought to its 8-bit form on the way, sums are fp32, the result is rounded once.  For an fp32 y the products are exact; for a
+ * bf16 y the 8-bit matrix instruction forms them, which drops what lies far below the largest product of its group:
+ * 5e-6 of a result row's norm for values of a normal distribution, 5e-5 for values of every exponent, where y's own rounding is 2e-3.
+ * n <= 2^22, k <= 2^20, m <= 2^19, m n <= 2^36.  scratch: pat_op_f8_gemm_scratch_bytes() bytes, 256-byte aligned, overwritten.  y must not overlap x. */
 int64_t pat_op_f8_weight_bytes(int32_t n, int32_t k);
 int64_t pat_op_f8_scale_bytes(int32_t n, int32_t k);
 int pat_op_f8_pack_weight(const void *w, int32_t type, int64_t ld, int32_t n, int32_t k, void *packed, void *scales, void *hip_stream);

@@ -142,7 +142,8 @@ __global__ __launch_bounds__(kPlan) void attn_plan_kernel(SharedPlanArgs a)
         if (cost < least) { least = cost; c = 32 * t; }
     }
     const int64_t room = 2 * (int64_t)n + 512;                 // chunks beyond the first of each group's members, or sequence
-    const int CP = max(c * kW, up(pp / room + 1, kTile * kW)), CS = max(solo ? c : c * kW, up(ws / room + 1, kTile));
+    const int64_t most = 1 << 29;                              // a chunk's end stays an int; lengths are at most 2^30
+    const int CP = max(c * kW, up(min(pp / room + 1, most), kTile * kW)), CS = max(solo ? c : c * kW, up(min(ws / room + 1, most), kTile));
 
     for (int g = tid; g < ng; g += kPlan) {
         const int members = bad_groups ? 0 : a.group_start[g + 1] - a.group_start[g];
@@ -252,11 +253,12 @@ __device__ __forceinline__ bool stream_keys(const SharedArgs &a, const SharedRec
     const int lane = threadIdx.x & 63, col = lane & 15, g4 = lane >> 4;
     const int G = a.hq / a.hkv, lgP = a.lgP, P = 1 << lgP;
     const int last = e.t0 + e.cnt - 1, tb = e.t0 & ~15, tiles = (last - tb) / kTile + 1;
-    const int n = tiles > w0 ? (tiles - w0 + ws - 1) / ws : 0;
+    const bool beyond = (last >> lgP) >= a.max_pages;          // keys that no page holds: nothing of the record is read, its rows are no number
+    const int n = tiles > w0 && !beyond ? (tiles - w0 + ws - 1) / ws : 0;
     const int64_t page_bytes = (int64_t)(a.hkv << lgP) * D * 2, head_bytes = (int64_t)(h << lgP) * D * 2;
     const char *kpool = reinterpret_cast<const char *>(a.k) + head_bytes, *vpool = reinterpret_cast<const char *>(a.v) + head_bytes;
     const uint32_t to = lds_offset(ring);
-    bool bad = false;
+    bool bad = beyond;
     int page = 0;
     // lane i holds the page of half i % 2 (16 keys lie in one page) of the wave's tile (i / 2) of the next 32
     auto look_up = [&](int i0) {

@@ -38,7 +38,7 @@ extern "C" {
 
 int pat_op_rope_table(int64_t n_pos, int32_t head_dim, double base, float *cos_sin, void *stream)
 {
-    if (!cos_sin || !aligned(cos_sin, 16) || n_pos <= 0 || n_pos > (1 << 30) || (head_dim != 64 && head_dim != 128) || !(base > 1.0)) return PAT_EINVAL;
+    if (!cos_sin || !aligned(cos_sin, 16) || n_pos <= 0 || n_pos > (1 << 25) || (head_dim != 64 && head_dim != 128) || !(base > 1.0)) return PAT_EINVAL;
     return done(launch_rope_table(cos_sin, n_pos, head_dim, base, (hipStream_t)stream));
 }
 
@@ -53,7 +53,7 @@ int pat_op_kv_append(const void *qkv, int32_t type, int64_t ld, int32_t rows, in
     if (!qkv || !seq || !pos || !cos_sin || !k_pages || !v_pages || !page_table || !q_out || n_pos <= 0 || n_seqs <= 0 || max_pages <= 0) return PAT_EINVAL;
     if (ld < width || ldq < (int64_t)n_q_heads * head_dim || ld * el % 16 || ldq * el % 16) return PAT_EINVAL;
     if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(cos_sin, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16)) return PAT_EINVAL;
-    if ((gq == nullptr) != (gk == nullptr) || !(eps >= 0.f) || rows * (width / head_dim) >= ((int64_t)1 << 31)) return PAT_EINVAL;
+    if ((gq == nullptr) != (gk == nullptr) || !(eps >= 0.f) || rows * (width / head_dim) >= ((int64_t)1 << 28)) return PAT_EINVAL;     // up to 16 lanes a head, below 2^32 of them
     AppendArgs a{};
     a.qkv = qkv; a.q_out = q_out; a.ld = ld; a.ldq = ldq; a.k = (uint16_t *)k_pages; a.v = (uint16_t *)v_pages;
     a.seq = seq; a.pos = pos; a.page_table = page_table; a.cs = cos_sin; a.gq = (const uint16_t *)gq; a.gk = (const uint16_t *)gk; a.skipped = skipped;
@@ -114,7 +114,7 @@ int pat_op_f8_pack_weight(const void *w, int32_t type, int64_t ld, int32_t n, in
     return done(launch_f8_pack_weight(w, type == PAT_F32, ld, n, k, packed, scales, (hipStream_t)stream));
 }
 
-static bool batch_ok(int32_t n, int32_t k, int32_t m) { return product_ok(n, k) && m >= 0 && m <= (1 << 19); }
+static bool batch_ok(int32_t n, int32_t k, int32_t m) { return product_ok(n, k) && m >= 0 && m <= (1 << 19) && (int64_t)m * n <= ((int64_t)1 << 36); }
 
 static int64_t part_offset(int32_t m, int32_t k) { return (f8_act_bytes(m, k) + f8_act_scale_bytes(m, k) + 255) / 256 * 256; }
 

@@ -51,7 +51,9 @@ struct SharedHeader {
 constexpr int32_t kSharedMark = 0x50415453;
 inline int64_t shared_plan_bytes(int n_seqs, int G)
 {
-    return (int64_t)sizeof(SharedHeader) + n_seqs * (int64_t)sizeof(SharedSeq) + shared_records(n_seqs, G) * (int64_t)sizeof(SharedRecord);
+    // at least a SharedSeq for as many sequences as any plan has: a call made with a plan for fewer reads its own, and finds out, inside the buffer
+    const int64_t used = n_seqs * (int64_t)sizeof(SharedSeq) + shared_records(n_seqs, G) * (int64_t)sizeof(SharedRecord), least = kSharedMaxSeqs * (int64_t)sizeof(SharedSeq);
+    return (int64_t)sizeof(SharedHeader) + (used > least ? used : least);
 }
 struct SharedPlanArgs {
     const int32_t *kv_len, *group_start, *shared_len;

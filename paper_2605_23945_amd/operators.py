@@ -153,7 +153,7 @@ def pat_op_attn_shared(q, k_pages, v_pages, page_table, plan, out=None):
 
 def pat_op_f8_pack_weight(w):
     """w [n, k] fp32 or bf16 -> (packed, scales): its 8-bit form, uint8 tensors as pat_op_f8_gemm reads them."""
-    _need(w.dim() == 2 and w.dtype in _TYPE and w.stride(1) == 1, "w: fp32 or bf16 [n, k], rows dense")
+    _need(w.dim() == 2 and w.dtype in _TYPE and (w.stride(1) == 1 or w.shape[1] == 1), "w: fp32 or bf16 [n, k], rows dense")
     n, k = w.shape
     dev, lib = _one_device(w), load_library()
     nbytes, sbytes = lib.pat_op_f8_weight_bytes(n, k), lib.pat_op_f8_scale_bytes(n, k)
@@ -165,7 +165,7 @@ def pat_op_f8_pack_weight(w):
 
 def pat_op_f8_gemm(packed, scales, n, x, y=None, mode=0, y_dtype=None):
     """y [m, n] = (mode 0) or += (mode 1) x W^T for x [m, k] and the packed W [n, k]; y's type is x's unless y or y_dtype says otherwise."""
-    _need(x.dim() == 2 and x.dtype in _TYPE and x.stride(1) == 1, "x: fp32 or bf16 [m, k], rows dense")
+    _need(x.dim() == 2 and x.dtype in _TYPE and (x.stride(1) == 1 or x.shape[1] == 1), "x: fp32 or bf16 [m, k], rows dense")
     m, k = x.shape
     dev, lib = _one_device(x, packed, scales, y), load_library()
     if packed.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or packed.numel() != lib.pat_op_f8_weight_bytes(n, k) or scales.numel() != lib.pat_op_f8_scale_bytes(n, k) \
@@ -174,7 +174,7 @@ def pat_op_f8_gemm(packed, scales, n, x, y=None, mode=0, y_dtype=None):
     if y is None:
         _need(mode == 0, "mode 1 adds to a given y")
         y = torch.empty(m, n, dtype=y_dtype or x.dtype, device=dev)
-    if y.dtype not in _TYPE or y.shape != (m, n) or y.stride(1) != 1:
+    if y.dtype not in _TYPE or y.shape != (m, n) or (y.stride(1) != 1 and n > 1):
         _need(False, f"y: fp32 or bf16 [{m}, {n}], rows dense")
     nbytes = lib.pat_op_f8_gemm_scratch_bytes(n, k, m)
     _need(nbytes >= 0, "x: more rows than a call takes")

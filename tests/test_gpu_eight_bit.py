@@ -121,6 +121,14 @@ def test_adding_to_y_and_rows_with_strides(pat, m, n, k, dtype):
     assert torch.equal(y[:, :2].cpu(), yw[:, :2]) and torch.equal(y[:, n + 2:].cpu(), yw[:, n + 2:])
 
 
+def test_single_columns_of_any_stride(pat):
+    w, x = _x((40, 1), 1), _x((5, 1), 2)
+    w2, x2 = w.t().contiguous().t(), x.t().contiguous().t()    # [n, 1] with strides (1, n)
+    assert torch.equal(_run(pat, x2, w2), _run(pat, x, w))
+    y = torch.full((1, 5), float("nan"), device=DEV).t()       # and a result of one column
+    assert torch.equal(_run(pat, x2, w2[:1], y=y), _run(pat, x, w[:1])) and not bool(y.isnan().any())
+
+
 def test_no_rows(pat):
     pw = pat.pat_op_f8_pack_weight(_x((32, 64), 1).to(DEV))
     assert pat.pat_op_f8_gemm(*pw, 32, torch.empty(0, 64, device=DEV)).shape == (0, 32)

@@ -197,6 +197,34 @@ def test_impossible_lengths_groups_and_pages_give_nan(pat):
     assert bool(pat.pat_op_attn_shared(b.q.to(DEV), b.k, b.v, _i32(b.table), plan).isnan().all())
 
 
+def test_a_plan_made_for_fewer_sequences_gives_nan(pat):
+    plan = pat.pat_op_attn_plan(_i32([5]), _i32([0, 1]), _i32([0]), 5, 4, 4, 64)
+    wide = pat.pat_op_attn_plan(_i32([5] * 2048), _i32([0, 2048]), _i32([0]), 5, 4, 4, 64)
+    wide.buf = plan.buf
+    k = torch.zeros(1, 4, 16, 64, dtype=torch.bfloat16, device=DEV)
+    got = pat.pat_op_attn_shared(torch.ones(2048, 4, 64, device=DEV), k, k.clone(), _i32([[0]] * 2048), wide)
+    assert bool(got.isnan().all())
+
+
+@pytest.mark.parametrize("hq,hkv", [(4, 4), (130, 1)])
+def test_lengths_far_beyond_the_table(pat, hq, hkv):
+    """The longest length a plan takes, with pages for a few tokens: no number for those, at once, and the others' results as they are."""
+    b = Batch([(20, [30, 25]), (0, [40]), (5, [9, 21])], hq, hkv, 64, 16, torch.bfloat16)
+    top = 1 << 30
+    for lens, shared, good in (([30, 25, top, 9, 21], [20, 0, 5], [0, 1, 3, 4]), ([top, top, 40, 9, 21], [top, 0, 5], [2, 3, 4]), ([top, top - 1, top, top, top], [20, 0, 5], [])):
+        plan = pat.pat_op_attn_plan(_i32(lens), _i32(b.start), _i32(shared), top, hq, hkv, 64)
+        got = pat.pat_op_attn_shared(b.q.to(DEV), b.k, b.v, _i32(b.table), plan)
+        b.check(got, rows=good)
+        assert bool(got[[s for s in range(5) if s not in good]].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_out_in_place_of_q(pat, dtype):
+    b = Batch([(41, [50, 43, 60]), (0, [7])], 8, 2, 128, 16, dtype)
+    q = b.q.to(DEV)
+    b.check(b.run(pat, q=q, out=q))
+
+
 def test_captured_step_follows_the_lengths(pat):
     """Plan and attention in one graph: replays with grown lengths, other work between them, each against the eager result."""
     b = Batch([(60, [75 + i for i in range(6)]), (0, [20])], 8, 2, 64, 16, torch.bfloat16, seed=11)

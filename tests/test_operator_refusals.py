@@ -22,7 +22,7 @@ APPEND = dict(qkv=P, type=0, ld=12 * 64, rows=0, hq=4, hkv=4, d=64, seq=P, pos=P
 @pytest.mark.parametrize("bad", [dict(rows=-1), dict(type=2), dict(hq=0), dict(hkv=0), dict(hq=5000), dict(d=96), dict(page=48), dict(page=256), dict(n_pages=0), dict(ld=700), dict(ldq=255),
                                  dict(ld=12 * 64 + 2), dict(ldq=4 * 64 + 1), dict(type=1, ld=12 * 64 + 4), dict(qkv=None), dict(seq=None), dict(pos=None), dict(cs=None),
                                  dict(k=None), dict(v=None), dict(table=None), dict(q=None), dict(qkv=P + 4), dict(q=P + 8), dict(k=P + 2), dict(v=P + 8), dict(cs=P + 4), dict(n_pos=0),
-                                 dict(n_seqs=0), dict(max_pages=0), dict(gq=P), dict(gk=P), dict(eps=-1.0), dict(eps=float("nan")), dict(rows=1 << 30)])
+                                 dict(n_seqs=0), dict(max_pages=0), dict(gq=P), dict(gk=P), dict(eps=-1.0), dict(eps=float("nan")), dict(rows=1 << 30), dict(rows=(1 << 28) // 12 + 1)])
 def test_append_refuses(lib, bad):
     a = dict(APPEND, **{"rows": 1, **bad})
     assert lib.pat_op_kv_append(*a.values()) == EINVAL
@@ -32,7 +32,7 @@ def test_append_of_nothing_is_fine(lib):
     assert lib.pat_op_kv_append(*APPEND.values()) == OK
 
 
-@pytest.mark.parametrize("bad", [(0, 64, 1e4, P), (16, 96, 1e4, P), (16, 64, 1.0, P), (16, 64, float("nan"), P), (16, 64, 1e4, None), (16, 64, 1e4, P + 4), (1 << 31, 64, 1e4, P)])
+@pytest.mark.parametrize("bad", [(0, 64, 1e4, P), (16, 96, 1e4, P), (16, 64, 1.0, P), (16, 64, float("nan"), P), (16, 64, 1e4, None), (16, 64, 1e4, P + 4), (1 << 31, 64, 1e4, P), ((1 << 25) + 1, 64, 1e4, P)])
 def test_rope_table_refuses(lib, bad):
     assert lib.pat_op_rope_table(*bad, None) == EINVAL
 
@@ -58,6 +58,8 @@ def test_attention_sizes(lib):
     assert lib.pat_op_attn_plan_bytes(0, 8, 2) == -1 and lib.pat_op_attn_plan_bytes(4, 8, 3) == -1 and lib.pat_op_attn_plan_bytes(2049, 8, 2) == -1
     assert lib.pat_op_attn_scratch_bytes(4, 8, 2, 96) == -1 and lib.pat_op_attn_scratch_bytes(4, 7, 2, 64) == -1
     assert 0 < lib.pat_op_attn_plan_bytes(4, 8, 2) < lib.pat_op_attn_plan_bytes(4, 128, 2)       # more heads than a row block holds: more records
+    # a call with a plan made for fewer sequences reads inside the plan
+    assert min(lib.pat_op_attn_plan_bytes(n, 8, 2) for n in (1, 7, 300, 2048)) >= 2048 * 32
     # a part per sequence and chunk: room for all sequences' shared and own ones beside the chunks
     assert lib.pat_op_attn_scratch_bytes(2048, 8, 2, 64) >= 2 * 2048 * 8 * 66 * 4
 
@@ -73,7 +75,7 @@ def test_weight_packing_refuses(lib, bad):
 
 
 @pytest.mark.parametrize("bad", [dict(w=None), dict(ws=None), dict(x=None), dict(y=None), dict(scratch=None), dict(x_type=2), dict(y_type=-1), dict(ldx=255), dict(ldy=31), dict(mode=2), dict(mode=-1),
-                                 dict(m=-1), dict(m=(1 << 19) + 1), dict(n=0), dict(k=0), dict(w=P + 128), dict(ws=P + 1), dict(x=P + 1), dict(y=P + 2), dict(scratch=P + 16)])
+                                 dict(m=-1), dict(m=(1 << 19) + 1), dict(n=0), dict(k=0), dict(w=P + 128), dict(ws=P + 1), dict(x=P + 1), dict(y=P + 2), dict(scratch=P + 16), dict(n=(1 << 17) + 1, ldy=(1 << 17) + 1, m=1 << 19)])
 def test_product_refuses(lib, bad):
     assert lib.pat_op_f8_gemm(*dict(GEMM, **bad).values()) == EINVAL
 
@@ -86,6 +88,7 @@ def test_product_sizes(lib):
     assert lib.pat_op_f8_weight_bytes(1, 1) == 2048 and lib.pat_op_f8_weight_bytes(17, 129) == 4 * 2048 and lib.pat_op_f8_weight_bytes(0, 5) == -1
     assert lib.pat_op_f8_scale_bytes(1, 1) == 4 and lib.pat_op_f8_scale_bytes(129, 513) == 16 and lib.pat_op_f8_scale_bytes(5, 0) == -1
     assert lib.pat_op_f8_gemm_scratch_bytes(5, 5, -1) == -1 and lib.pat_op_f8_gemm_scratch_bytes(5, 5, 0) == 0
+    assert lib.pat_op_f8_gemm_scratch_bytes((1 << 17) + 1, 5, 1 << 19) == -1
     for n, k, m in ((4096, 11008, 251), (64, 28672, 100), (32000, 128, 70)):       # x's 8-bit form, its scales, the slices' sums
         need = -(-m // 16) * 16 * (-(-k // 512) * 512 + -(-k // 512) * 4)
         assert lib.pat_op_f8_gemm_scratch_bytes(n, k, m) >= need
