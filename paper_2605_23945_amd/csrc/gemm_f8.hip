@@ -512,14 +512,16 @@ hipError_t launch_tile(const F8Args &a, int slices, hipStream_t s)
     return hipGetLastError();
 }
 
-// tiles of a workgroup: as few as leave one workgroup per compute unit
+// Tiles of a workgroup: as few as leave one workgroup per compute unit, up to three.  27 rows of 5120 x 6912 by 1, 2 and 3 tiles: 18.1, 15.3 and 16.3 us; of 22016 x 4096: 27.7,
+// 24.0 and 22.4; one row of 12288 x 4096: 13.7, 14.3 and 11.2.  fp32 results of four batch tiles leave no registers for three (60 rows of 12288 x 4096: 29.8 us, 23.2 by two).
 template <int MB, bool RAW, typename X, typename E>
 hipError_t launch_stream(const F8Args &a, const X *x, int64_t ldx, int k, bool vec, hipStream_t s)
 {
+    constexpr int kMost = MB == 4 && sizeof(E) == 4 ? 2 : 3;
     const int NT = (a.n + 15) / 16;
     if (NT <= 256) f8_stream_kernel<MB, 1, RAW, X, E><<<NT, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
-    else if (NT <= 512) f8_stream_kernel<MB, 2, RAW, X, E><<<(NT + 1) / 2, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
-    else f8_stream_kernel<MB, 3, RAW, X, E><<<(NT + 2) / 3, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
+    else if (NT <= 512 || kMost == 2) f8_stream_kernel<MB, 2, RAW, X, E><<<(NT + 1) / 2, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
+    else f8_stream_kernel<MB, kMost, RAW, X, E><<<(NT + kMost - 1) / kMost, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
     return hipGetLastError();
 }
 
