@@ -12,7 +12,13 @@
 // for another while it streams.  Both products run on the matrix cores with a row per operand column:
 //   S^T[key, row] = K q^T,   O^T[feature, row] += V^T p^T    (V read transposed from LDS)
 // q is exact in one bf16 term where it is bf16 and in three where it is fp32; p = h + l to 2^-16 in two truncated terms beside
-// bf16 outputs (whose own rounding is 2^-9), and exact in three beside fp32 ones.  K's and V's fragments serve two row tiles.
+// bf16 outputs (whose own rounding is 2^-9), and exact in three beside fp32 ones.  K's and V's fragments serve two row tiles of a bf16 record;
+// fp32 ones take their tiles in turn.
+//
+// What bounds it: K's and V's bytes where there are many.  256 sequences of 16 groups on 32 KV heads (1.98 GB): 326 us and 6.6 for the join, 6.1 TB/s, the
+// rate of plain reads; 64 sequences on one prefix of 8190 keys and 20 KV heads (302 MB): 55 and 4.6 us.  Small ones are a chain of dependent steps: the record, q and
+// the pages (1.5 us), the first K (3 us), its tiles, the waves' meeting, the join's launch: three sequences of 50 keys 4.6 and 3.9 us, 128 on one KV head with fp32
+// queries (56 MB) 22 and 4.  The plan takes 13 to 16 us, once for all of a step's layers.
 #include "attn_mfma_dev.h"
 #include "pat_ops.h"
 
