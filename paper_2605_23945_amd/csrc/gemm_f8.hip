@@ -208,11 +208,11 @@ __device__ __forceinline__ floatx4_t mfma_f8(v8i_t a, v8i_t b, floatx4_t c, int 
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, S, sa, S, sb);
 }
 
-// eight 8-bit values as bf16, exactly
-__device__ __forceinline__ bf16x8_t widen8(int lo, int hi)
+// eight 8-bit values as bf16, exactly, times a power of two
+__device__ __forceinline__ bf16x8_t widen8(int lo, int hi, float scale = 1.0f)
 {
-    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-    const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 // a block's product by the bf16 instructions, scaled and added: |sum| 2^(both exponents) as a product of powers of two is exact
@@ -446,9 +446,27 @@ __global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, 
             if (u == 0) load_scales(cn, kb + 4);
             load_batch(b[(u + 3) & 3], kb + u + 3);
             const int sw = c.w >> (8 * u), sw2 = c.w2 >> (8 * u);
+            // fp32 results: x widened once for all weight tiles (they are of one block of 128 rows), and the factor 2^(both exponents) of the block's sums: what of
+            // it an fp32 number does not hold goes into the widened x, whose sums are then beyond the result's range in any case
+            bf16x8_t xw[WIDE ? TM : 1][4];
+            float by[WIDE ? TM : 1];
+            if constexpr (WIDE) {
+                static_assert(8 % TN == 0, "a workgroup's weight tiles have one scale");
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const int e = (int)(c.x[i] >> (8 * u) & 255) + (sw & 255) - 254, r = min(max(e, -126), 127), rest = max(e - r, -126);
+                    const float f = __uint_as_float((uint32_t)(rest + 127) << 23);
+                    const v8i_t xv = both(b[u].lo[i], b[u].hi[i]);
+                    by[i] = __uint_as_float((uint32_t)(r + 127) << 23);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xw[i][j] = widen8(xv[2 * j], xv[2 * j + 1], f);
+                }
+            }
 #pragma unroll
             for (int t = 0; t < TN; ++t) {
-                __builtin_amdgcn_sched_barrier(0);             // or all of the block's weights are read ahead, into registers that the sums need
+                // or all of the block's weights are read ahead, into registers that the sums need; fp32 results' four tiles leave room, and their chains of four
+                // products per tile go on side by side (100 x 12288 x 4096: 28.7 us with the fence, 26.3 without)
+                if constexpr (!WIDE) __builtin_amdgcn_sched_barrier(0);
                 if (t + kAhead == TN) {
                     // newer than the next block's weights: x of S - 1 blocks, weights of S - 2, and the scales where they were among them
                     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"((S - 1) * 2 * TM + (S - 2) * NJ + (u < S - 1 ? TM + 2 : 0)) : "memory");
@@ -463,9 +481,15 @@ __global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, 
                 const int s = t < edge ? sw : sw2;
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
-                    const v8i_t xv = both(b[u].lo[i], b[u].hi[i]);
-                    const int sx = c.x[i] >> (8 * u);
-                    acc[t][i] = WIDE ? mfma_wide(wv, xv, acc[t][i], s, sx) : mfma_f8<0>(wv, xv, acc[t][i], s, sx);
+                    if constexpr (WIDE) {
+                        floatx4_t p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(wv[2 * j], wv[2 * j + 1]), xw[i][j], p, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[t][i][j] = fmaf(p[j], by[i], acc[t][i][j]);
+                    } else {
+                        acc[t][i] = mfma_f8<0>(wv, both(b[u].lo[i], b[u].hi[i]), acc[t][i], s, (int)(c.x[i] >> (8 * u)));
+                    }
                 }
             }
         }
@@ -554,7 +578,7 @@ hipError_t launch_product(const F8Args &a, hipStream_t s)
 
 // Weight tiles and waves of a workgroup and cuts of K.  A workgroup keeps a compute unit about as busy as two do, so the time is rounds of
 // 256 workgroups, blocks of columns in each and a block's time: 0.36, 0.55 and 0.75 us for 4, 8 and 12 tiles by four waves, 1.0 and 1.37 us for 8 and 12 by eight
-// (measured on products of 100 to 5003 rows), 0.7 us for fp32 results; a cut K costs a launch and its sums' way out and back.  Measured, 5003 x 7168 x 8192: 12 tiles by
+// (measured on products of 100 to 5003 rows), 0.7 us for fp32 results (0.63 measured: what a cut costs them is a little less than the rule says); a cut K costs a launch and its sums' way out and back.  Measured, 5003 x 7168 x 8192: 12 tiles by
 // eight waves 269 us, by four 286, 8 tiles 287 and 295; 2048 x 8192 x 8192: 155, 139, 125 and 136; 128 x 22016 x 4096: 40, 31, 32 and 27, 4 tiles 31;
 // 100 x 12288 x 4096: 35, 26, 25 and 20, 4 tiles 16; 251 x 4096 x 11008: two slices of 4 tiles 26, four of 8 27, one of 4 37.  The rule takes the best of each.
 F8Tile f8_tile(int n, int m, int KB, bool wide)

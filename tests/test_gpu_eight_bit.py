@@ -90,6 +90,21 @@ def test_scales_of_all_sizes(pat):
         assert torch.equal(_run(pat, t, eye).cpu().double(), eight_bit(t, 1)), e
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 130, 200), (40, 130, 200), (140, 130, 200)])
+def test_scales_of_all_sizes_in_products(pat, m, n, k):
+    """Exponents of x and W that cancel, or leave a large or a small result, and one whose scales' product is no fp32 number."""
+    for ex, ew in ((-110, 110), (110, -110), (60, 50), (-60, -50), (-100, 20), (-126, 0), (-70, -70), (0, 118)):
+        x, w = (_x((m, k), 5).clamp(-3, 3) * 2.0 ** ex), (_x((n, k), 6).clamp(-3, 3) * 2.0 ** ew)
+        got = _run(pat, x, w)
+        xq, wq = eight_bit(x, 1), eight_bit(w, 128)
+        ref, allow = project(xq, wq)
+        check(got, ref, allow + k * 2.0 ** -149)               # and a step of fp32's smallest numbers for each sum
+    x, w = torch.full((m, k), 2.0 ** 100), torch.full((n, k), -2.0 ** 90)
+    assert bool((_run(pat, x, w) == float("-inf")).all())      # 2^190
+    x, w = torch.full((m, k), 2.0 ** -100), torch.full((n, k), 2.0 ** -90)
+    assert not bool(_run(pat, x, w).any())                     # 2^-190
+
+
 def test_what_is_not_finite_becomes_nan_and_leaves_the_scale_alone(pat):
     x = _x((3, 256), 2)
     x[1, 5], x[2, 200] = float("inf"), float("nan")
