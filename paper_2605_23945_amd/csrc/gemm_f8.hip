@@ -370,6 +370,8 @@ __global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, 
     constexpr int TM = kBatchTiles, kStage = TN * 2048, NJ = 2 * TN / W;      // load instructions of a wave per stage
     constexpr int kAhead = 3;                                  // weight tiles in registers on their way from LDS: one tile's products are shorter than its read
     constexpr bool WIDE = sizeof(E) == 4;
+    constexpr bool kTwo = 8 % TN != 0;                         // a workgroup's weight tiles may be of two blocks of 128 rows: two words of scales
+    constexpr int kScales = TM + 1 + kTwo;                     // load instructions of load_scales
     __shared__ __align__(16) char lds[S * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int KB4 = (a.KB + 3) / 4, NT = (a.n + 15) / 16, MT = a.Mp / 16;
@@ -417,7 +419,8 @@ __global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, 
         const int at = min(kb >> 2, KB4 - 1);
 #pragma unroll
         for (int i = 0; i < TM; ++i) c.x[i] = xss[i][(int64_t)at * a.Mp];
-        c.w = wss[at]; c.w2 = wss2[at];
+        c.w = wss[at];
+        if constexpr (kTwo) c.w2 = wss2[at];
     };
     auto pin = [&](Batch &b) {                                 // here, or the compiler waits for newer loads than it needs to later
 #pragma unroll
@@ -445,13 +448,13 @@ __global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, 
         for (int u = 0; u < 4; ++u) {
             if (u == 0) load_scales(cn, kb + 4);
             load_batch(b[(u + 3) & 3], kb + u + 3);
-            const int sw = c.w >> (8 * u), sw2 = c.w2 >> (8 * u);
+            const int sw = c.w >> (8 * u), sw2 = kTwo ? (int)(c.w2 >> (8 * u)) : sw;
             // fp32 results: x widened once for all weight tiles (they are of one block of 128 rows), and the factor 2^(both exponents) of the block's sums: what of
             // it an fp32 number does not hold goes into the widened x, whose sums are then beyond the result's range in any case
             bf16x8_t xw[WIDE ? TM : 1][4];
             float by[WIDE ? TM : 1];
             if constexpr (WIDE) {
-                static_assert(8 % TN == 0, "a workgroup's weight tiles have one scale");
+                static_assert(!kTwo, "a workgroup's weight tiles have one scale");
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
                     const int e = (int)(c.x[i] >> (8 * u) & 255) + (sw & 255) - 254, r = min(max(e, -126), 127), rest = max(e - r, -126);
@@ -468,8 +471,9 @@ __global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, 
                 // products per tile go on side by side (100 x 12288 x 4096: 28.7 us with the fence, 26.3 without)
                 if constexpr (!WIDE) __builtin_amdgcn_sched_barrier(0);
                 if (t + kAhead == TN) {
-                    // newer than the next block's weights: x of S - 1 blocks, weights of S - 2, and the scales where they were among them
-                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"((S - 1) * 2 * TM + (S - 2) * NJ + (u < S - 1 ? TM + 2 : 0)) : "memory");
+                    // newer than the next block's weights: x of S - 1 blocks, weights of S - 2, and the scales where they were among them.
+                    // One too many would let a wave read weights that have not arrived; this wait alone holds them back.
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"((S - 1) * 2 * TM + (S - 2) * NJ + (u < S - 1 ? kScales : 0)) : "memory");
                     pin(b[(u + 1) & 3]);
                     asm volatile("s_barrier" ::: "memory");
                     fetch(kb + u + S, slot);
@@ -478,7 +482,7 @@ __global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, 
                 if (t + kAhead < TN) weight(slot, t + kAhead, wf[(t + kAhead) & 3]);
                 else weight(slot, t + kAhead - TN, wf[(t + kAhead) & 3]);
                 const v8i_t wv = both(wf[t & 3][0], wf[t & 3][1]);
-                const int s = t < edge ? sw : sw2;
+                const int s = !kTwo || t < edge ? sw : sw2;
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
                     if constexpr (WIDE) {
@@ -495,7 +499,7 @@ __global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, 
         }
         c = cn;
     }
-    static_assert(TN % 4 == 0 && (S - 1) * 2 * TM + (S - 2) * NJ + TM + 2 <= 63, "the next block's first weights land where this step's begin; the counter has six bits");
+    static_assert(TN % 4 == 0 && (S - 1) * 2 * TM + (S - 2) * NJ + kScales <= 63, "the next block's first weights land where this step's begin; the counter has six bits");
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // nothing may arrive in LDS that has gone to another workgroup
     if (slices > 1) {                                          // fp32 sums of the slice: [slice][batch row][weight row]
         float *part = a.part + (int64_t)sl * a.Mp * NT * 16;
