@@ -11,8 +11,8 @@
 // 128 features), the K half requested anew as soon as its fragments are in registers, the V half likewise, so no wave waits
 // for another while it streams.  Both products run on the matrix cores with a row per operand column:
 //   S^T[key, row] = K q^T,   O^T[feature, row] += V^T p^T    (V read transposed from LDS)
-// q is exact in one bf16 term where it is bf16 and in three where it is fp32; p = h + l to 2^-16 in two truncated terms beside
-// bf16 outputs (whose own rounding is 2^-9), and exact in three beside fp32 ones.  K's and V's fragments serve two row tiles of a bf16 record;
+// q is exact in one bf16 term where it is bf16 and in three where it is fp32; p to 2^-17 in two rounded terms beside bf16 outputs
+// (whose own rounding is 2^-8), and exact in three beside fp32 ones.  K's and V's fragments serve two row tiles of a bf16 record;
 // fp32 ones take their tiles in turn.
 //
 // What bounds it: K's and V's bytes where there are many.  256 sequences of 16 groups on 32 KV heads (1.98 GB): 326 us and 6.6 for the join, 6.1 TB/s, the
@@ -226,6 +226,8 @@ __device__ __forceinline__ float column_max(float v)
     return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
 }
 
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) { return (uint32_t)f32_to_bf16(a) | ((uint32_t)f32_to_bf16(b) << 16); }
+
 template <bool F32> struct QTerms { static constexpr int n = F32 ? 3 : 1, p = F32 ? 3 : 2; };
 
 // eight consecutive features of a query row as operand terms
@@ -237,14 +239,15 @@ __device__ __forceinline__ void load_q(const float *p, u32x4_t (&t)[3])
     split3_bf16(v, t[0], t[1], t[2]);
 }
 
-// p as two bf16 terms, each truncated: p - h - m < 2^-16 p
+// p as two bf16 terms, each rounded to nearest: p - h - m is at most 2^-17 p, of either sign.  (Truncated terms, as many instructions and the same times, leave up to
+// 2^-15 p and every result 1e-5 short in the mean: the sum that it is divided by is of whole p's.)
 __device__ __forceinline__ void split2_bf16(const float *p, u32x4_t &h, u32x4_t &m)
 {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         const float x = p[2 * w], y = p[2 * w + 1];
-        const float xr = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u), yr = y - __uint_as_float(__float_as_uint(y) & 0xFFFF0000u);
-        h[w] = upper_halves(x, y); m[w] = upper_halves(xr, yr);
+        h[w] = two_bf16(x, y);
+        m[w] = two_bf16(x - bf16lo(h[w]), y - bf16hi(h[w]));
     }
 }
 
