@@ -91,6 +91,10 @@ int64_t pat_op_f8_weight_bytes(int32_t n, int32_t k);
 int64_t pat_op_f8_scale_bytes(int32_t n, int32_t k);
 int pat_op_f8_pack_weight(const void *w, int32_t type, int64_t ld, int32_t n, int32_t k, void *packed, void *scales, void *hip_stream);
 int64_t pat_op_f8_gemm_scratch_bytes(int32_t n, int32_t k, int32_t m);
+/* The kernel that pat_op_f8_gemm launches (diagnostics, host only): plan[0] 0 the streaming product with x as it is, 1 the same after x was brought to its 8-bit
+ * form, 2 the product by tiles (more than 64 rows); plan[1], plan[2] tiles of 16 rows of W and of x per workgroup, plan[3] its waves, plan[4] cuts of k.
+ * Returns PAT_EINVAL for sizes or types that pat_op_f8_gemm refuses, and for m = 0. */
+int pat_op_f8_gemm_plan(int32_t n, int32_t k, int32_t m, int32_t x_type, int32_t y_type, int32_t plan[5]);
 int pat_op_f8_gemm(const void *w_packed, const void *w_scales, int32_t n, int32_t k, const void *x, int32_t x_type, int64_t ldx, int32_t m,
                    void *y, int32_t y_type, int64_t ldy, int32_t mode, void *scratch, void *hip_stream);
 

@@ -90,7 +90,7 @@ EXPORTS = ["pat_decode_query", "pat_decode_init", "pat_load_layer", "pat_load_la
            "pat_predictor_fit", "pat_predictor_destroy", "pat_predictor_line", "pat_predictor_query", "pat_switch_decide",
            "pat_kv_move_seconds", "pat_rms_length", "pat_profile_plan",
            "pat_op_rope_table", "pat_op_kv_append", "pat_op_attn_plan_bytes", "pat_op_attn_scratch_bytes", "pat_op_attn_plan", "pat_op_attn_shared",
-           "pat_op_f8_weight_bytes", "pat_op_f8_scale_bytes", "pat_op_f8_pack_weight", "pat_op_f8_gemm_scratch_bytes", "pat_op_f8_gemm"]
+           "pat_op_f8_weight_bytes", "pat_op_f8_scale_bytes", "pat_op_f8_pack_weight", "pat_op_f8_gemm_scratch_bytes", "pat_op_f8_gemm_plan", "pat_op_f8_gemm"]
 
 _lib = None
 
@@ -169,6 +169,7 @@ def load_library() -> C.CDLL:
     lib.pat_op_attn_plan.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
     lib.pat_op_attn_shared.argtypes = [vp, i32, i64, i32, i32, i32, i32, vp, vp, i32, i32, vp, i32, vp, vp, i64, vp, vp]
     lib.pat_op_f8_pack_weight.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp]
+    lib.pat_op_f8_gemm_plan.argtypes = [i32, i32, i32, i32, i32, i32p]
     lib.pat_op_f8_gemm.argtypes = [vp, vp, i32, i32, vp, i32, i64, i32, vp, i32, i64, i32, vp, vp]
     for name, n in (("pat_op_attn_plan_bytes", 3), ("pat_op_attn_scratch_bytes", 4), ("pat_op_f8_weight_bytes", 2), ("pat_op_f8_scale_bytes", 2),
                     ("pat_op_f8_gemm_scratch_bytes", 3)):

@@ -549,13 +549,15 @@ hipError_t launch_tile(const F8Args &a, int slices, hipStream_t s)
 
 // Tiles of a workgroup: as few as leave one workgroup per compute unit, up to three.  27 rows of 5120 x 6912 by 1, 2 and 3 tiles: 18.1, 15.3 and 16.3 us; of 22016 x 4096: 27.7,
 // 24.0 and 22.4; one row of 12288 x 4096: 13.7, 14.3 and 11.2.  fp32 results of four batch tiles leave no registers for three (60 rows of 12288 x 4096: 29.8 us, 23.2 by two).
+constexpr int stream_most(int MB, bool wide) { return MB == 4 && wide ? 2 : 3; }
+
 template <int MB, bool RAW, typename X, typename E>
 hipError_t launch_stream(const F8Args &a, const X *x, int64_t ldx, int k, bool vec, hipStream_t s)
 {
-    constexpr int kMost = MB == 4 && sizeof(E) == 4 ? 2 : 3;
-    const int NT = (a.n + 15) / 16;
-    if (NT <= 256) f8_stream_kernel<MB, 1, RAW, X, E><<<NT, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
-    else if (NT <= 512 || kMost == 2) f8_stream_kernel<MB, 2, RAW, X, E><<<(NT + 1) / 2, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
+    constexpr int kMost = stream_most(MB, sizeof(E) == 4);
+    const int NT = (a.n + 15) / 16, TN = f8_stream_tiles(a.n, MB, sizeof(E) == 4);
+    if (TN == 1) f8_stream_kernel<MB, 1, RAW, X, E><<<NT, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
+    else if (TN == 2) f8_stream_kernel<MB, 2, RAW, X, E><<<(NT + 1) / 2, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
     else f8_stream_kernel<MB, kMost, RAW, X, E><<<(NT + kMost - 1) / kMost, kStreamWaves * 64, 0, s>>>(a, x, ldx, k, vec);
     return hipGetLastError();
 }
@@ -579,6 +581,12 @@ hipError_t launch_product(const F8Args &a, hipStream_t s)
 }
 
 }  // namespace
+
+int f8_stream_tiles(int n, int MB, bool wide)
+{
+    const int NT = (n + 15) / 16, most = stream_most(MB, wide);
+    return NT <= 256 ? 1 : NT <= 512 ? 2 : most;
+}
 
 // Weight tiles and waves of a workgroup and cuts of K.  A workgroup keeps a compute unit about as busy as two do, so the time is rounds of
 // 256 workgroups, blocks of columns in each and a block's time: 0.36, 0.55 and 0.75 us for 4, 8 and 12 tiles by four waves, 1.0 and 1.37 us for 8 and 12 by eight

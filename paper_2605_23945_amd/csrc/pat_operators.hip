@@ -123,6 +123,20 @@ int64_t pat_op_f8_gemm_scratch_bytes(int32_t n, int32_t k, int32_t m)
     return batch_ok(n, k, m) ? part_offset(m, k) + f8_part_bytes(n, m, k) : -1;
 }
 
+int pat_op_f8_gemm_plan(int32_t n, int32_t k, int32_t m, int32_t x_type, int32_t y_type, int32_t plan[5])
+{
+    if (!plan || !batch_ok(n, k, m) || m == 0 || !type_ok(x_type) || !type_ok(y_type)) return PAT_EINVAL;
+    const bool wide = y_type == PAT_F32;
+    if (m <= 64) {
+        plan[0] = f8_takes_raw(m, k, x_type == PAT_F32) ? 0 : 1;
+        plan[2] = (m + 15) / 16; plan[1] = f8_stream_tiles(n, plan[2], wide); plan[3] = 8; plan[4] = 1;
+        return PAT_OK;
+    }
+    const F8Tile t = f8_tile(n, m, (k + 127) / 128, wide);
+    plan[0] = 2; plan[1] = t.TN; plan[2] = 2 * t.W; plan[3] = t.W; plan[4] = t.slices;
+    return PAT_OK;
+}
+
 int pat_op_f8_gemm(const void *w_packed, const void *w_scales, int32_t n, int32_t k, const void *x, int32_t x_type, int64_t ldx, int32_t m, void *y,
                    int32_t y_type, int64_t ldy, int32_t mode, void *scratch, void *stream)
 {
@@ -136,9 +150,7 @@ int pat_op_f8_gemm(const void *w_packed, const void *w_scales, int32_t n, int32_
     a.y = y; a.ldy = ldy; a.n = n; a.m = m; a.Mp = (m + 15) / 16 * 16; a.KB = (k + 127) / 128; a.add = mode == 1;
     a.part = (float *)((char *)scratch + part_offset(m, k));
     a.vec = aligned(y, 4 * size_of(y_type)) && ldy % 4 == 0;
-    // Every workgroup reads x whole.  Up to 64 KiB of it the product's waves bring it to 8 bits themselves (one row of 4096 x 12288: 11.4 us, 12.8 with a launch
-    // before it); above, what that costs each workgroup passes the launch (16 rows of 4096 x 22016: 22.2 and 19.8 us).
-    if (m <= 16 && (int64_t)m * k * size_of(x_type) <= 65536) return done(launch_f8_gemm_raw(a, x, x_type == PAT_F32, ldx, k, y_type == PAT_F32, (hipStream_t)stream));
+    if (f8_takes_raw(m, k, x_type == PAT_F32)) return done(launch_f8_gemm_raw(a, x, x_type == PAT_F32, ldx, k, y_type == PAT_F32, (hipStream_t)stream));
     const hipError_t e = launch_f8_pack_act(x, x_type == PAT_F32, ldx, m, k, scratch, sc, (hipStream_t)stream);
     return e != hipSuccess ? PAT_EHIP : done(launch_f8_gemm(a, y_type == PAT_F32, (hipStream_t)stream));
 }
