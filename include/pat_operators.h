@@ -59,7 +59,7 @@ int pat_op_kv_append(const void *qkv, int32_t type, int64_t ld, int32_t rows, in
  *
  * pat_op_attn_plan cuts the step's work from the lengths on the device; its result serves every layer's pat_op_attn_shared
  * until a length changes.  group_start is int32[n_groups + 1] from 0 to n_seqs, ascending (equal values: an empty group);
- * n_seqs and n_groups <= 2048.  plan: pat_op_attn_plan_bytes() bytes, 16-byte aligned.  A kv_len[s] below 0 or above max_len, or
+ * n_seqs and n_groups 1 .. 2048 (a step without sequences has nothing to call).  plan: pat_op_attn_plan_bytes() bytes, 16-byte aligned.  A kv_len[s] below 0 or above max_len, or
  * group_start that is no such list, gives NaN as the result of the sequence, or of all, and so does a page id outside
  * [0, n_pages) or a length beyond max_pages, of the sequences that need the page.
  *

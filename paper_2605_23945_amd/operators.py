@@ -119,16 +119,20 @@ class AttnPlan:
 def pat_op_attn_plan(kv_len, group_start, shared_len, max_len, n_q_heads, n_kv_heads, head_dim, plan=None):
     """The plan of one step for sequences of kv_len[s] <= max_len cached tokens (int32 [n]), of which group_start[g] .. group_start[g + 1] - 1 share
     their first shared_len[g] tokens (int32 [groups + 1] and [groups]).  plan: one to write anew (of as many sequences and the same heads), as a
-    captured graph does."""
+    captured graph does.  No sequences (a drained step): a plan by which the attention does nothing."""
     n, ng = kv_len.shape[0], shared_len.shape[0]
     dev = _one_device(kv_len, group_start, shared_len)
-    _need(1 <= n <= PAT_ATTN_MAX_SEQS and 1 <= ng <= PAT_ATTN_MAX_SEQS, f"1 .. {PAT_ATTN_MAX_SEQS} sequences and groups")
+    _need(n <= PAT_ATTN_MAX_SEQS and ng <= PAT_ATTN_MAX_SEQS and (n == 0 or ng > 0), f"up to {PAT_ATTN_MAX_SEQS} sequences and groups, a group at least for any sequence")
     if plan is None:
-        lib = load_library()
-        nbytes, scratch = lib.pat_op_attn_plan_bytes(n, n_q_heads, n_kv_heads), lib.pat_op_attn_scratch_bytes(n, n_q_heads, n_kv_heads, head_dim)
+        lib, most = load_library(), max(n, 1)
+        nbytes, scratch = lib.pat_op_attn_plan_bytes(most, n_q_heads, n_kv_heads), lib.pat_op_attn_scratch_bytes(most, n_q_heads, n_kv_heads, head_dim)
         _need(nbytes > 0 and scratch > 0, f"{n_q_heads} query heads on {n_kv_heads} KV heads of {head_dim} features")
-        plan = AttnPlan(torch.empty(nbytes, dtype=torch.uint8, device=dev), n, n_q_heads, n_kv_heads, head_dim, scratch)
+        plan = AttnPlan(torch.empty(nbytes if n else 0, dtype=torch.uint8, device=dev), n, n_q_heads, n_kv_heads, head_dim, scratch)
     _need((plan.n_seqs, plan.hq, plan.hkv, plan.d, plan.buf.device) == (n, n_q_heads, n_kv_heads, head_dim, dev), "plan: made for other sequences or heads, or on another device")
+    if n == 0:
+        for t, size, what in ((kv_len, 0, "kv_len"), (group_start, ng + 1, "group_start"), (shared_len, ng, "shared_len")):
+            _list(t, size, what)
+        return plan
     _call(dev, "pat_op_attn_plan", _list(kv_len, n, "kv_len"), _list(group_start, ng + 1, "group_start"), _list(shared_len, ng, "shared_len"), n, ng,
           max_len, n_q_heads, n_kv_heads, plan.buf.data_ptr())
     return plan
@@ -145,6 +149,9 @@ def pat_op_attn_shared(q, k_pages, v_pages, page_table, plan, out=None):
     if out is None:
         out = torch.empty(n, hq, d, dtype=q.dtype, device=dev)
     _need(out.dtype == q.dtype and out.shape[0] == n, "out: of q's type and rows")
+    if n == 0:
+        _rows(out, hq, d, "out")
+        return out
     scratch = torch.empty(plan.scratch_bytes, dtype=torch.uint8, device=dev)
     _call(dev, "pat_op_attn_shared", q.data_ptr(), _TYPE[q.dtype], ldq, n, hq, hkv, d, k_pages.data_ptr(), v_pages.data_ptr(), n_pages, P,
           page_table.data_ptr(), max_pages, plan.buf.data_ptr(), out.data_ptr(), _rows(out, hq, d, "out"), scratch.data_ptr())
