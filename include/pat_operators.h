@@ -39,7 +39,7 @@ int pat_op_rope_table(int64_t n_pos, int32_t head_dim, double base, float *cos_s
  * v heads of the token of sequence seq[i] at position pos[i]: one row per sequence in a decode step, many where prompts are
  * prefilled, in any order.  With gains gq, gk (bf16 [head_dim], both or neither) each q and k head first gets an RMSNorm
  * with epsilon eps.  q and k heads are rotated: features (j, j + head_dim / 2) by the angle of (pos[i], j).  q goes to row i of
- * q_out [rows, ldq] in qkv's type (it may be qkv itself with ldq = ld), k and v rounded to the cache.
+ * q_out [rows, ldq] in qkv's type (it may be qkv itself with ldq = ld; other overlaps are refused), k and v rounded to the cache.
  *   16-byte alignment: qkv, q_out, cos_sin, the pools, and ld and ldq in bytes.  rows * (heads of a row) < 2^28.
  *   seq[i] < 0 is a row of padding: nothing is read or written for it.
  *   seq[i] >= n_seqs, pos[i] outside [0, n_pos) or the table's row, a page id outside [0, n_pages): nothing is written for the row,
@@ -86,7 +86,7 @@ int pat_op_attn_shared(const void *q, int32_t type, int64_t ldq, int32_t n_seqs,
  * brought to its 8-bit form on the way, sums are fp32, the result is rounded once.  For an fp32 y the products are exact; for a
  * bf16 y the 8-bit matrix instruction forms them, which drops what lies far below the largest product of its group:
  * 5e-6 of a result row's norm for values of a normal distribution, 5e-5 for values of every exponent, where y's own rounding is 2e-3.
- * n <= 2^22, k <= 2^20, m <= 2^19, m n <= 2^36.  scratch: pat_op_f8_gemm_scratch_bytes() bytes, 256-byte aligned, overwritten.  y must not overlap x. */
+ * n <= 2^22, k <= 2^20, m <= 2^19, m n <= 2^36.  scratch: pat_op_f8_gemm_scratch_bytes() bytes, 256-byte aligned, overwritten.  y must not overlap x: such a call is refused. */
 int64_t pat_op_f8_weight_bytes(int32_t n, int32_t k);
 int64_t pat_op_f8_scale_bytes(int32_t n, int32_t k);
 int pat_op_f8_pack_weight(const void *w, int32_t type, int64_t ld, int32_t n, int32_t k, void *packed, void *scales, void *hip_stream);

@@ -2,6 +2,7 @@
 // allocates, and everything is enqueued on the caller's stream, so the calls can be captured into a graph.
 #include "../../include/pat_operators.h"
 #include "pat_ops.h"
+#include "row_overlap.h"
 
 #include <atomic>
 
@@ -54,6 +55,8 @@ int pat_op_kv_append(const void *qkv, int32_t type, int64_t ld, int32_t rows, in
     if (ld < width || ldq < (int64_t)n_q_heads * head_dim || ld * el % 16 || ldq * el % 16) return PAT_EINVAL;
     if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(cos_sin, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16)) return PAT_EINVAL;
     if ((gq == nullptr) != (gk == nullptr) || !(eps >= 0.f) || rows * (width / head_dim) >= ((int64_t)1 << 28)) return PAT_EINVAL;     // up to 16 lanes a head, below 2^32 of them
+    const bool in_place = q_out == qkv && (ldq == ld || rows == 1);
+    if (!in_place && rows_overlap(qkv, ld * el, width * el, q_out, ldq * el, (int64_t)n_q_heads * head_dim * el, rows)) return PAT_EINVAL;
     AppendArgs a{};
     a.qkv = qkv; a.q_out = q_out; a.ld = ld; a.ldq = ldq; a.k = (uint16_t *)k_pages; a.v = (uint16_t *)v_pages;
     a.seq = seq; a.pos = pos; a.page_table = page_table; a.cs = cos_sin; a.gq = (const uint16_t *)gq; a.gk = (const uint16_t *)gk; a.skipped = skipped;
@@ -144,6 +147,7 @@ int pat_op_f8_gemm(const void *w_packed, const void *w_scales, int32_t n, int32_
     if (!w_packed || !w_scales || !aligned(w_packed, 256) || !aligned(w_scales, 4) || ldx < k || ldy < n) return PAT_EINVAL;
     if (m == 0) return PAT_OK;
     if (!x || !y || !scratch || !aligned(x, size_of(x_type)) || !aligned(y, size_of(y_type)) || !aligned(scratch, 256)) return PAT_EINVAL;
+    if (rows_overlap(x, ldx * size_of(x_type), k * size_of(x_type), y, ldy * size_of(y_type), n * size_of(y_type), m)) return PAT_EINVAL;
     char *sc = (char *)scratch + f8_act_bytes(m, k);
     F8Args a{};
     a.w = (const uint4 *)w_packed; a.x = (const uint4 *)scratch; a.ws = (const uint32_t *)w_scales; a.xs = (const uint32_t *)sc;
