@@ -40,7 +40,7 @@ int pat_op_rope_table(int64_t n_pos, int32_t head_dim, double base, float *cos_s
  * prefilled, in any order.  With gains gq, gk (bf16 [head_dim], both or neither) each q and k head first gets an RMSNorm
  * with epsilon eps.  q and k heads are rotated: features (j, j + head_dim / 2) by the angle of (pos[i], j).  q goes to row i of
  * q_out [rows, ldq] in qkv's type (it may be qkv itself with ldq = ld; other overlaps are refused), k and v rounded to the cache.
- *   16-byte alignment: qkv, q_out, cos_sin, the pools, and ld and ldq in bytes.  rows * (heads of a row) < 2^28.
+ *   16-byte alignment: qkv, q_out, cos_sin, the pools, and ld and ldq in bytes.  rows * (heads of a row) < 2^28 (fp32 heads of 128 features: < 2^28 - 15).
  *   seq[i] < 0 is a row of padding: nothing is read or written for it.
  *   seq[i] >= n_seqs, pos[i] outside [0, n_pos) or the table's row, a page id outside [0, n_pages): nothing is written for the row,
  *   and *skipped (device, or NULL) is raised by one.

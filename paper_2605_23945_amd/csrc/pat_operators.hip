@@ -54,7 +54,8 @@ int pat_op_kv_append(const void *qkv, int32_t type, int64_t ld, int32_t rows, in
     if (!qkv || !seq || !pos || !cos_sin || !k_pages || !v_pages || !page_table || !q_out || n_pos <= 0 || n_seqs <= 0 || max_pages <= 0) return PAT_EINVAL;
     if (ld < width || ldq < (int64_t)n_q_heads * head_dim || ld * el % 16 || ldq * el % 16) return PAT_EINVAL;
     if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(cos_sin, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16)) return PAT_EINVAL;
-    if ((gq == nullptr) != (gk == nullptr) || !(eps >= 0.f) || rows * (width / head_dim) >= ((int64_t)1 << 28)) return PAT_EINVAL;     // up to 16 lanes a head, below 2^32 of them
+    if ((gq == nullptr) != (gk == nullptr) || !(eps >= 0.f) || rows * (width / head_dim) >= ((int64_t)1 << 28) - (type == PAT_F32 && head_dim == 128 ? 15 : 0))
+        return PAT_EINVAL;                                     // up to 16 lanes a head, in workgroups of 256 below 2^32 of them
     const bool in_place = q_out == qkv && (ldq == ld || rows == 1);
     if (!in_place && rows_overlap(qkv, ld * el, width * el, q_out, ldq * el, (int64_t)n_q_heads * head_dim * el, rows)) return PAT_EINVAL;
     AppendArgs a{};
