@@ -15,10 +15,11 @@
 // (whose own rounding is 2^-8), and exact in three beside fp32 ones.  K's and V's fragments serve two row tiles of a bf16 record;
 // fp32 ones take their tiles in turn.
 //
-// What bounds it: K's and V's bytes where there are many.  256 sequences of 16 groups on 32 KV heads (1.98 GB): 326 us and 6.6 for the join, 6.1 TB/s, the
-// rate of plain reads; 64 sequences on one prefix of 8190 keys and 20 KV heads (302 MB): 55 and 4.6 us.  Small ones are a chain of dependent steps: the record, q and
-// the pages (1.5 us), the first K (3 us), its tiles, the waves' meeting, the join's launch: three sequences of 50 keys 4.6 and 3.9 us, 128 on one KV head with fp32
-// queries (56 MB) 22 and 4.  The plan takes 13 to 16 us, once for all of a step's layers.
+// What bounds it: K's and V's bytes where there are many.  256 sequences of 16 groups on 32 KV heads (1.98 GB): 325 us and 6.4 for the join, 6.1 TB/s, the
+// rate of plain reads; 64 sequences on one prefix of 8190 keys and 20 KV heads (302 MB): 54 and 4.6 us.  Small ones are a chain of dependent steps: the record, q and
+// the pages (1.5 us), the first K (3 us), its tiles, the waves' meeting, the join's launch; and a grid for all the records that a plan has room for, most of whose
+// workgroups find none: three sequences of 50 keys 4.8 and 3.9 us.  128 on one KV head with fp32 queries (56 MB): 22 and 4, where a record of more than 16 rows walks its
+// chain and its keys twice.  The plan takes 13 to 16 us, once for all of a step's layers.
 #include "attn_mfma_dev.h"
 #include "pat_ops.h"
 
@@ -611,7 +612,7 @@ hipError_t launch_shared(const SharedArgs &a, int n_cu, hipStream_t s)
     typedef typename std::conditional<F32, float, uint16_t>::type E;
     const int G = a.hq / a.hkv;
     const int64_t items = shared_records(a.n_seqs, G) * a.hkv;
-    const unsigned grid = (unsigned)(items < 16 * n_cu ? items : 16 * n_cu);
+    const unsigned grid = (unsigned)(items < 16 * n_cu ? items : 16 * n_cu);       // by the plan's room: how many items it has is known on the device alone
     attn_shared_kernel<D, F32><<<grid, kW * 64, kW * kTile * D * 4, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -4,7 +4,7 @@
 //   y[m, n] = sum over blocks b of 2^(ex[m, b] + ew[n / 128, b]) sum over k in b of qx[m, k] qw[n, k]
 // The matrix instruction of 16 x 16 x 128 8-bit operands takes both exponents per operand row and multiplies them in, so a block is one
 // instruction with nothing beside it, and sums stay in its fp32 accumulators.  It does not keep all bits of a block's smaller products
-// (5e-6 of the result's norm on values of a normal distribution, 5e-5 on values of every exponent): nothing beside a bf16 result's own 2^-9, and it
+// (5e-6 of the result's norm on values of a normal distribution, 5e-5 on values of every exponent): nothing beside a bf16 result's own 2^-8, and it
 // serves those.  For fp32 results the 8-bit values are widened to bf16 (exactly) and multiplied by the bf16 instructions, whose sums are fp32
 // throughout, at half the rate; a block's sum is then scaled and added.
 //
@@ -12,11 +12,10 @@
 // holds row r, columns half * 64 + g * 16 ..; lane g * 16 + r of a wave loads the pieces of both halves, 1 KiB per instruction.
 // (The instruction would have 32 consecutive columns in a lane; any order does that both operands share.)
 //
-// What bounds it: the weights' bytes for few rows.  One row of 12288 x 4096 (50 MB): 9.8 us, 5.1 TB/s, launch and ramp included, of 6.0 that plain
-// reads reach; 27 fp32 rows of 5120 x 6912: 12 us, and 3 before it for x, which every workgroup reads whole.  For many rows the way of the operands to the compute
-// units and the clock: 5003 rows of 7168 x 8192 238 us and 19 for x, together 2.25 PFLOP/s (a library product of 8192 cubed 2.8, of these sizes 1.8); without its matrix
-// products the same kernel takes 0.9 of its time, and they keep the pipes busy for 60 % of it.  251 rows of 22016 x 4096: 29 and 5 us, where weights and products need
-// 15 to 17 each.
+// What bounds it: the weights' bytes for few rows.  One row of 12288 x 4096 (50 MB): 9.9 us, 5.1 TB/s, launch and ramp included, of 6.0 that plain reads reach.  Where x
+// comes packed and for many rows, the loads that the compiler's waits leave under way (see both kernels): 27 fp32 rows of 5120 x 6912 take 12 us, and 3 before it for x, where
+// the bytes take 6; 251 rows of 22016 x 4096 30 and 4, where weights and products take 15 to 17 each; 5003 rows of 7168 x 8192 245 us and 19 for x, together 2.2 PFLOP/s
+// (a library product of 8192 cubed 2.8, of these sizes 1.8).
 #include "pat_dev.h"
 #include "pat_ops.h"
 
@@ -257,8 +256,9 @@ __device__ __forceinline__ void emit(const F8Args &a, int m, int n0, floatx4_t v
 
 // ---- few rows: weights streamed once, straight into registers ------------------------------------------------------
 // A workgroup holds TN tiles of 16 weight rows; its eight waves take the blocks of columns in turn (wave w: w, w + 8, ...) and their
-// sums meet in LDS, added in wave order.  A wave keeps three blocks' operands in registers (two above 32 rows), all but one of them on their way: a block's weights and its part of x
-// are requested together, since loads arrive in order.  Where x is small (RAW) every wave brings it to its 8-bit form
+// sums meet in LDS, added in wave order.  A wave has registers for three blocks' operands (two above 32 rows): a block's weights and its part of x are
+// requested together, two blocks (one) before they are multiplied.  Not all of that stays under way: packed x's scales are shifted right behind their request, for which
+// the compiler waits for everything but the newest block's weights, and where the paths around the last blocks meet it waits for all of them, once in three (two) blocks.  Where x is small (RAW) every wave brings it to its 8-bit form
 // itself, in the registers the product reads it from: lanes r, r + 16, r + 32 and r + 48 hold row r's block; no launch, no scratch and no barrier
 // precede the stream.  Elsewhere x comes packed.
 constexpr int kStreamWaves = 8;
@@ -358,12 +358,14 @@ __global__ __launch_bounds__(kStreamWaves * 64) void f8_stream_kernel(F8Args a, 
 // ---- many rows: tiles on the matrix cores ------------------------------------------------------------------------------
 // A workgroup of W waves holds TN tiles of 16 weight rows and 2 W tiles of 16 batch rows, a wave all TN and two of the batch's: weights go through LDS
 // (asynchronous loads, S stages of TN x 2 KiB), where the waves share them; the batch's tiles are one wave's alone and go straight to
-// registers, three blocks of columns ahead (x has just been written, so it comes from beyond the XCD's own L2).  Towards the end
+// registers, requested three blocks of columns ahead (x has just been written, so it comes from beyond the XCD's own L2).  Towards the end
 // of a block all waves meet: the next block's weights have arrived, and the stage just read is requested anew.  Loads arrive in order,
-// so a wave waits for its weights by the number of loads that it has issued since.
+// so a wave waits for its weights by the number of loads that it has issued since.  The compiler's wait for the next block's x counts its own loads alone, not those to LDS,
+// and so leaves 8 loads under way (12 where scales were requested), whatever S: x is ahead by about one block and the weights by less.  For fp32 results it also brings the
+// weights' scales to a scalar register where they are requested, once in four blocks, and waits for all loads but two there.
 // The loop takes four blocks a turn, which one word of scales covers; K is padded to that with blocks of x that are zero.  There is no branch
 // in it: the compiler moves matrix products past one.
-constexpr int kBatchTiles = 2;      // four: 287 us where two take 286 (5003 x 7168 x 8192), more at every smaller batch
+constexpr int kBatchTiles = 2;      // four, on 512 registers, 276 us where two take 261 (5003 x 7168 x 8192, x's launch included)
 template <int TN, int W, int S, typename E>
 __global__ __launch_bounds__(W * 64, 2) void f8_tile_kernel(F8Args a, int nblk, int mblk, int slices)
 {
@@ -547,8 +549,9 @@ hipError_t launch_tile(const F8Args &a, int slices, hipStream_t s)
     return hipGetLastError();
 }
 
-// Tiles of a workgroup: as few as leave one workgroup per compute unit, up to three.  27 rows of 5120 x 6912 by 1, 2 and 3 tiles: 18.1, 15.3 and 16.3 us; of 22016 x 4096: 27.7,
-// 24.0 and 22.4; one row of 12288 x 4096: 13.7, 14.3 and 11.2.  fp32 results of four batch tiles leave no registers for three (60 rows of 12288 x 4096: 29.8 us, 23.2 by two).
+// Tiles of a workgroup: as few as leave one workgroup per compute unit, up to three.  27 fp32 rows of 5120 x 6912 by 1, 2 and 3 tiles, x's launch included: 19.8, 17.3
+// and 19.0 us; of 22016 x 4096: 29.7, 28.5 and 25.8; one row of 12288 x 4096: 14.3, 15.4 and 12.2.  fp32 results of four batch tiles leave no registers for three
+// (60 rows of 12288 x 4096: 30 us, 24 by two).
 constexpr int stream_most(int MB, bool wide) { return MB == 4 && wide ? 2 : 3; }
 
 template <int MB, bool RAW, typename X, typename E>
@@ -590,9 +593,9 @@ int f8_stream_tiles(int n, int MB, bool wide)
 
 // Weight tiles and waves of a workgroup and cuts of K.  A workgroup keeps a compute unit about as busy as two do, so the time is rounds of
 // 256 workgroups, blocks of columns in each and a block's time: 0.36, 0.55 and 0.75 us for 4, 8 and 12 tiles by four waves, 1.0 and 1.37 us for 8 and 12 by eight
-// (measured on products of 100 to 5003 rows), 0.7 us for fp32 results (0.63 measured: what a cut costs them is a little less than the rule says); a cut K costs a launch and its sums' way out and back.  Measured, 5003 x 7168 x 8192: 12 tiles by
-// eight waves 269 us, by four 286, 8 tiles 287 and 295; 2048 x 8192 x 8192: 155, 139, 125 and 136; 128 x 22016 x 4096: 40, 31, 32 and 27, 4 tiles 31;
-// 100 x 12288 x 4096: 35, 26, 25 and 20, 4 tiles 16; 251 x 4096 x 11008: two slices of 4 tiles 26, four of 8 27, one of 4 37.  The rule takes the best of each.
+// (measured on products of 100 to 5003 rows), 0.7 us for fp32 results (0.63 measured: what a cut costs them is a little less than the rule says); a cut K costs a launch and its sums' way out and back.  Measured, x's launch included, 5003 x 7168 x 8192: 12 tiles by
+// eight waves 274 us, by four 283, 8 tiles 288 and 294; 2048 x 8192 x 8192: 161, 146, 130 and 144; 251 x 22016 x 4096: 48, 38, 39 and 47; 128 x 22016 x 4096: 45, 37, 34 and 33,
+// 4 tiles 35; 100 x 12288 x 4096: 41, 32, 30 and 28, 4 tiles 21; 251 x 4096 x 11008: two slices of 4 tiles 31, four of 8 31, one of 4 42.  The rule takes the best of each.
 F8Tile f8_tile(int n, int m, int KB, bool wide)
 {
     const int NT = (n + 15) / 16, KB4 = (KB + 3) / 4;

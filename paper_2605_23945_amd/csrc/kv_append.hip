@@ -8,7 +8,7 @@
 // What bounds it: memory.  A lane takes 16 bytes of a head's first half and the 16 bytes of their partners, so that a head is
 // 4 to 16 lanes, every access is 16 bytes wide (8 where fp32 becomes the cache's bf16), and the norm's sum is a few lane exchanges.
 // 10967 rows of 60 bf16 heads of 128 with the norm (338 MB read and written): 63 us, 5.3 TB/s, where a large copy reaches 5.0.  256 rows of 96 fp32
-// heads: 5.1 us, one row of 24: 2.2 us, which are a launch and one chain of dependent reads (sequence, page, data).
+// heads: 5.0 us, one row of 24: 2.5 us, which are a launch and one chain of dependent reads (sequence, page, data).
 #include "pat_dev.h"
 #include "pat_ops.h"
 

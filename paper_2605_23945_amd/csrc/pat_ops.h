@@ -87,8 +87,8 @@ struct F8Args {
     bool add, vec;             // y += ; rows n .. n + 3 of y by one store
     float *part;               // sums of K slices [slice][Mp][16-row tiles of n][16], where f8_tile has more than one
 };
-// Every workgroup of a product of few rows reads x whole.  Up to 64 KiB of it the product's waves bring it to 8 bits themselves (one row of 4096 x 12288: 11.4 us, 12.8
-// with a launch before it); above, what that costs each workgroup passes the launch (16 rows of 4096 x 22016: 22.2 and 19.8 us).
+// Every workgroup of a product of few rows reads x whole.  Up to 64 KiB of it the product's waves bring it to 8 bits themselves (one row of 12288 x 4096: 12.2 us, 13.5
+// with a launch before it); above, what that costs each workgroup passes the launch (16 rows of 12288 x 4096 13.5 and 13.4 us, of 4096 x 22016 31.5 and 22.4).
 inline bool f8_takes_raw(int m, int k, bool x32) { return m <= 16 && (int64_t)m * k * (x32 ? 4 : 2) <= 65536; }
 int f8_stream_tiles(int n, int MB, bool wide);        // up to 64 rows: tiles of weight rows per workgroup, for MB tiles of batch rows
 struct F8Tile { int TN, W, slices; };      // above 64 rows: tiles of weight rows per workgroup, waves of 32 batch rows, cuts of K
