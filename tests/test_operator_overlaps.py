@@ -20,7 +20,7 @@ PROGRAM = r"""
 // every placing of two operands' rows in one buffer, against its bytes
 int main()
 {
-    const int cases[][5] = {{1, 4, 4, 4, 4}, {3, 4, 12, 4, 12}, {3, 4, 12, 8, 12}, {4, 2, 6, 2, 6}, {3, 4, 12, 3, 5}, {5, 1, 3, 2, 7}, {2, 8, 8, 8, 16}, {6, 1, 9, 1, 4}, {6, 3, 4, 1, 11}};
+    const int cases[][5] = {{1, 4, 4, 4, 4}, {3, 4, 12, 4, 12}, {3, 4, 12, 8, 12}, {4, 2, 6, 2, 6}, {3, 4, 12, 3, 5}, {5, 1, 3, 2, 7}, {2, 8, 8, 8, 16}, {2, 8, 16, 8, 16}, {5, 3, 7, 2, 7}, {1, 3, 9, 5, 9}, {6, 1, 9, 1, 4}, {6, 3, 4, 1, 11}};
     long yes = 0, no = 0;
     for (auto &c : cases) {
         const int m = c[0], wa = c[1], la = c[2], wb = c[3], lb = c[4], at = 200;
@@ -53,6 +53,24 @@ def test_overlaps_are_found_byte_for_byte(tmp_path):
     assert r.returncode == 0, r.stdout
     yes, no = map(int, r.stdout.split())
     assert yes > 100 and no > 100
+
+
+@pytest.mark.skipif(not shutil.which("g++"), reason="no g++")
+def test_rows_side_by_side_are_told_apart_at_once(tmp_path):
+    """2^19 rows of x and y in one buffer, a thousand times: a walk over the rows would take seconds."""
+    src, exe = tmp_path / "many.cpp", tmp_path / "many"
+    src.write_text(r"""
+#include "row_overlap.h"
+int main()
+{
+    const char *p = reinterpret_cast<const char *>(0x100000);
+    int found = 0;
+    for (int i = 0; i < 1000; ++i) found += pat::rows_overlap(p, 4096, 1024, p + 1024 + i, 4096, 2048, 1 << 19);
+    return found;
+}
+""")
+    subprocess.run(["g++", "-std=c++17", "-O0", "-I" + CSRC, str(src), "-o", str(exe)], check=True, timeout=120)
+    assert subprocess.run([str(exe)], timeout=2).returncode == 0
 
 
 # x is 4 rows of 256 bf16 at P, y 4 rows of 32 fp32
